@@ -169,6 +169,99 @@ int dma_attn_fwd_ex(const void* q, const void* k, const void* v, void* out,
 /* Device scratch the forward needs beyond its inputs and output: always 0. */
 size_t dma_attn_fwd_workspace_bytes(int B, int Hq, int Hkv, int S, int D);
 
+/*
+ * A paged key / value cache in 8 bits, and the attention that reads it.
+ *
+ * Keys and values are held as MX elements (E4M3 or E5M2) in pages of `page_tokens` consecutive positions.  Every page of
+ * every kv head has ONE E8M0 scale for its keys and one for its values (value = element * 2^(scale - 127)); both fit bf16
+ * without rounding.  Values lie with the positions innermost, as the second product of the attention reads them.
+ *
+ *   k_codes     [num_pages, Hkv, page_tokens, D] bytes, 16-byte aligned
+ *   v_codes     [num_pages, Hkv, D, page_tokens] bytes, 16-byte aligned
+ *   k_scales, v_scales   [num_pages, Hkv] bytes
+ *   page_table  [B, max_pages] int32, 4-byte aligned: the page that holds positions [j * page_tokens, (j + 1) * page_tokens)
+ *               of sequence b is page_table[b][j].  An entry outside [0, num_pages) is no page: nothing is written to it,
+ *               and its positions do not exist for a reader.
+ *   page_tokens 16, 32, 64, 128 or 256.   D: 64 or 128.   fmt: DMA_FMT_MXFP8_E4M3 or DMA_FMT_MXFP8_E5M2.
+ *               max_pages * page_tokens must stay below 2^30, the bytes of k_codes below 2^40 (else DMA_ERR_UNSUPPORTED).
+ * All pointers are device memory of the caller; the structure itself is host memory and read during the call only.
+ */
+typedef struct dma_kv_cache {
+    void* k_codes;
+    void* v_codes;
+    void* k_scales;
+    void* v_scales;
+    const void* page_table;
+    int64_t num_pages;
+    int max_pages;
+    int page_tokens;
+    int Hkv;
+    int D;
+    int fmt;
+} dma_kv_cache;
+
+/* A bf16 tensor [B, heads, N, D] whose rows of D elements are dense and lie where the strides (in elements) say: token n of
+ * head h of sequence b starts at data + b * stride_batch + h * stride_head + n * stride_token.  data is 16-byte aligned and
+ * the strides are multiples of 8 (both so that a row can be read 16 bytes at a time) and not negative. */
+typedef struct dma_rows {
+    void* data;
+    int64_t stride_batch;
+    int64_t stride_head;
+    int64_t stride_token;
+} dma_rows;
+
+/*
+ * What the calls on a cache share.  Every one speaks of N tokens per sequence: token i of sequence b stands at position
+ * start[b] + i, and only the first n_tokens[b] of them exist (the rows behind them are neither read nor written: a padded
+ * batch keeps them).
+ *   B >= 0, N >= 0 (0 is a no-op).  N < 2^30.
+ *   start      [B] int32, device, 4-byte aligned.  A sequence with a negative start has no tokens.
+ *   n_tokens   [B] int32, device, 4-byte aligned, or NULL: N for every sequence.  Counts outside [0, N] are clamped to it.
+ * start, n_tokens and the page table are read by the kernels, so a captured graph follows their values from replay to replay.
+ */
+
+/*
+ * Writes the keys and values of new tokens to the cache.
+ *   k, v   [B, Hkv, N, D] bf16.
+ * The scale of a page is the smallest byte s with max|x| <= 1.75 * 2^e_max * 2^(s - 127) over the page's finite elements
+ * (e_max = 8 for E4M3, 15 for E5M2: the largest element is 1.75 * 2^e_max, so no finite element saturates), but at least 17
+ * and at most 246 (E4M3) or 239 (E5M2): every element times its scale is then a normal bf16 number or zero.  Elements are
+ * rounded to nearest even; an infinity becomes the largest element, a NaN stays one.
+ * A page whose first written position is not its first one holds earlier tokens: its scale stays where it suffices for the new
+ * tokens.  Where it does not, the scale grows and the earlier codes are rounded once more, to element * 2^(old - new) (exact
+ * but for what becomes subnormal).  A page that is written from its first position on takes its scale from the new tokens alone,
+ * whatever it held.  What a page holds behind the last token written is not kept.
+ * Positions past max_pages * page_tokens are dropped.  Two sequences that write to the same page in one call: unspecified.
+ */
+int dma_kv_write(const dma_kv_cache* cache, const dma_rows* k, const dma_rows* v, int B, int N, const void* start_i32,
+                 const void* n_tokens_i32, void* stream);
+
+/*
+ * Reads keys and values back: k_out, v_out [B, Hkv, N, D] bf16 receive element * 2^(scale - 127), exactly.  Rows of positions
+ * that do not exist (behind n_tokens, without a page, past max_pages * page_tokens) are left as they were.
+ */
+int dma_kv_read(const dma_kv_cache* cache, const dma_rows* k_out, const dma_rows* v_out, int B, int N, const void* start_i32,
+                const void* n_tokens_i32, void* stream);
+
+/*
+ * Attention over the cache: out = softmax(q k^T / sqrt(D)) v, the cache holding the keys and values of the query tokens
+ * themselves (dma_kv_write comes first).
+ *   q, out  [B, Hq, N, D] bf16; Hq % Hkv == 0, query head h reads kv head h / (Hq / Hkv).
+ *   The query at position p sees the keys at positions t <= p and, if window > 0, of these only t > p - window and
+ *   t < sink_tokens (the first tokens of the sequence stay visible).  window = 0: no window, sink_tokens has no effect.
+ *   A query that sees no key (none of the positions it could see has a page) gives zeros.
+ *   Positions that are not seen may hold anything, NaN codes among it.
+ * Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 for the second product, as in dma_attn_fwd.
+ * Equal calls give equal bits; the order of the sums over the keys follows from the sizes and the values of start and n_tokens.
+ *   workspace  device, 16-byte aligned, at least dma_cache_attn_workspace_bytes(...) bytes (NULL if that is 0); not
+ *              initialised by the caller, without meaning after the call.  Calls that may run at the same time need one each.
+ */
+int dma_cache_attn(const dma_kv_cache* cache, const dma_rows* q, const dma_rows* out, int B, int Hq, int N, const void* start_i32,
+                   const void* n_tokens_i32, int window, int sink_tokens, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of a dma_cache_attn call of these sizes on the current device; 0 also for sizes that the call refuses. */
+size_t dma_cache_attn_workspace_bytes(int B, int Hq, int Hkv, int N, int D);
+
 /* Diagnostic, not part of the method: plain device-to-device copy kernel (16 bytes per lane, no reuse) of `bytes`
  * bytes (a multiple of 16; src, dst 16-byte aligned, device, non-overlapping).  Its exactly known traffic (bytes read +
  * bytes written) is what the HBM byte counters of a profiler run are scaled by. */

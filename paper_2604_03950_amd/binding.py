@@ -18,7 +18,7 @@ FMT_MXFP4_E2M1 = 2
 FMT_MXFP8_E5M2 = 3
 
 EXPORTS = ("dma_mx_quantize", "dma_mx_quantize_token", "dma_mx_quantize_dual", "dma_mx_group_amax", "dma_attn_fwd", "dma_attn_fwd_ex",
-           "dma_attn_fwd_workspace_bytes", "dma_diag_copy", "dma_diag_mfma", "dma_diag_pipes", "dma_error_string", "dma_version")
+           "dma_attn_fwd_workspace_bytes", "dma_kv_write", "dma_kv_read", "dma_cache_attn", "dma_cache_attn_workspace_bytes", "dma_diag_copy", "dma_diag_mfma", "dma_diag_pipes", "dma_error_string", "dma_version")
 
 PIPE_IDLE, PIPE_MFMA_BF16, PIPE_MFMA_FP4, PIPE_MFMA_FP8, PIPE_FMA, PIPE_EXP, PIPE_CVT_PK_BF16 = range(7)
 
@@ -36,6 +36,16 @@ class AttnOpts(ctypes.Structure):
     _fields_ = [("tile", ctypes.c_int), ("sink_tiles", ctypes.c_int), ("pv_fmt", ctypes.c_int),
                 ("per_token_scale", ctypes.c_int), ("q_group_amax", ctypes.c_void_p), ("k_group_amax", ctypes.c_void_p),
                 ("fp8_mfma", ctypes.c_int)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("num_pages", ctypes.c_int64), ("max_pages", ctypes.c_int), ("page_tokens", ctypes.c_int),
+                ("Hkv", ctypes.c_int), ("D", ctypes.c_int), ("fmt", ctypes.c_int)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_batch", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_token", ctypes.c_int64)]
 
 
 def lib_path() -> str:
@@ -64,6 +74,15 @@ def load() -> ctypes.CDLL:
         L.dma_attn_fwd_ex.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, ctypes.POINTER(AttnOpts), vp]
         L.dma_attn_fwd_workspace_bytes.restype = ctypes.c_size_t
         L.dma_attn_fwd_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+        pc, pr = ctypes.POINTER(_Cache), ctypes.POINTER(_Rows)
+        L.dma_kv_write.restype = ci
+        L.dma_kv_write.argtypes = [pc, pr, pr, ci, ci, vp, vp, vp]
+        L.dma_kv_read.restype = ci
+        L.dma_kv_read.argtypes = [pc, pr, pr, ci, ci, vp, vp, vp]
+        L.dma_cache_attn.restype = ci
+        L.dma_cache_attn.argtypes = [pc, pr, pr, ci, ci, ci, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
+        L.dma_cache_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.dma_cache_attn_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
         L.dma_diag_copy.restype = ci
         L.dma_diag_copy.argtypes = [vp, vp, i64, vp]
         L.dma_diag_mfma.restype = ci
@@ -225,6 +244,131 @@ def dma_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, diag_band
     if rc:
         raise DmaError(rc, "dma_attn_fwd")
     return out
+
+
+class KVCache:
+    """Handle of a paged 8-bit key / value cache (``dma_kv_cache`` of the header) over tensors of the caller, all on one GPU:
+    k_codes [pages, Hkv, P, D], v_codes [pages, Hkv, D, P], k_scales and v_scales [pages, Hkv] uint8, page_table [B, max_pages]
+    int32.  It holds the tensors, nothing else; page_table's values may be changed at any time between calls."""
+
+    def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                 page_table: torch.Tensor, fmt: int = FMT_MXFP8_E4M3):
+        if k_codes.dim() != 4 or page_table.dim() != 2:
+            raise ValueError("k_codes must be [pages, Hkv, P, D], page_table [B, max_pages]")
+        pages, Hkv, P, D = k_codes.shape
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
+        self.page_table, self.fmt, self.device = page_table, int(fmt), k_codes.device
+        self.Hkv, self.D, self.page_tokens = Hkv, D, P
+        self.B, max_pages = page_table.shape
+        self._c = _Cache(_dev(k_codes, torch.uint8, "k_codes"), _dev(v_codes, torch.uint8, "v_codes", (pages, Hkv, D, P)),
+                         _dev(k_scales, torch.uint8, "k_scales", (pages, Hkv)), _dev(v_scales, torch.uint8, "v_scales", (pages, Hkv)),
+                         _dev(page_table, torch.int32, "page_table"), pages, max_pages, P, Hkv, D, int(fmt))
+        if any(t.device != self.device for t in (v_codes, k_scales, v_scales, page_table)):
+            raise ValueError("the tensors of a cache must be on one GPU")
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def empty(cls, page_table: torch.Tensor, num_pages: int, Hkv: int, D: int, page_tokens: int = 64,
+              fmt: int = FMT_MXFP8_E4M3) -> "KVCache":
+        """A cache of num_pages pages that hold nothing yet, on page_table's GPU."""
+        mk = lambda *shape: torch.empty(shape, dtype=torch.uint8, device=page_table.device)
+        return cls(mk(num_pages, Hkv, page_tokens, D), mk(num_pages, Hkv, D, page_tokens), mk(num_pages, Hkv), mk(num_pages, Hkv),
+                   page_table, fmt)
+
+
+def _rows(t: torch.Tensor, what: str, shape, device) -> _Rows:
+    """A bf16 tensor [B, heads, N, D] whose rows are dense, at any strides the library takes (it checks them)."""
+    if t.dtype != torch.bfloat16 or t.device != device or t.shape != shape:
+        raise ValueError(f"{what}: need a torch.bfloat16 tensor {tuple(shape)} on the cache's GPU")
+    sb, sh, sn, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"{what}: the last dimension must be dense")
+    # a dimension of one element has no stride to speak of
+    return _Rows(t.data_ptr(), sb if shape[0] > 1 else 0, sh if shape[1] > 1 else 0, sn if shape[2] > 1 else 0)
+
+
+def _spans(cache: KVCache, start: torch.Tensor, n_tokens: torch.Tensor | None):
+    """Pointers of start and n_tokens.  The call goes to the current stream, which has to be one of the cache's GPU."""
+    device = cache.device
+    if device.index != (_current_device or torch.cuda.current_device)():
+        raise ValueError(f"the cache is on {device}, which is not the current device")
+    if start.device != device or start.shape != (cache.B,):
+        raise ValueError(f"start: need [{cache.B}] on the cache's GPU")
+    if n_tokens is None:
+        return _dev(start, torch.int32, "start"), None
+    if n_tokens.device != device:
+        raise ValueError("n_tokens: need it on the cache's GPU")
+    return _dev(start, torch.int32, "start"), _dev(n_tokens, torch.int32, "n_tokens", (cache.B,))
+
+
+def dma_kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor, n_tokens: torch.Tensor | None = None) -> None:
+    """Quantizes k, v [B, Hkv, N, D] bf16 (any strides with dense rows) into the cache: token i of sequence b at position
+    start[b] + i, the first n_tokens[b] of them (all by default); start, n_tokens: int32 [B] on the GPU."""
+    ps, pn = _spans(cache, start, n_tokens)
+    if k.dim() != 4:
+        raise ValueError("k must be [B, Hkv, N, D]")
+    N = k.shape[2]
+    shape = (cache.B, cache.Hkv, N, cache.D)
+    rk, rv = _rows(k, "k", shape, cache.device), _rows(v, "v", shape, cache.device)
+    rc = load().dma_kv_write(cache._ref, rk, rv, cache.B, N, ps, pn, _stream())
+    if rc:
+        raise DmaError(rc, "dma_kv_write")
+
+
+def dma_kv_read(cache: KVCache, start: torch.Tensor, N: int | None = None, n_tokens: torch.Tensor | None = None, out=None):
+    """Reads positions start[b] + [0, n_tokens[b]) back: (k, v) [B, Hkv, N, D] bf16.  Rows that do not exist are left as they
+    were in out = (k, v), whose token dimension then gives N; without out they are zeros."""
+    ps, pn = _spans(cache, start, n_tokens)
+    if out is None:
+        if N is None:
+            raise ValueError("N or out is needed")
+        out = tuple(torch.zeros((cache.B, cache.Hkv, N, cache.D), dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    k, v = out
+    if k.dim() != 4 or (N is not None and k.shape[2] != N):
+        raise ValueError("out must be two tensors [B, Hkv, N, D]")
+    N = k.shape[2]
+    shape = (cache.B, cache.Hkv, N, cache.D)
+    rk, rv = _rows(k, "k", shape, cache.device), _rows(v, "v", shape, cache.device)
+    rc = load().dma_kv_read(cache._ref, rk, rv, cache.B, N, ps, pn, _stream())
+    if rc:
+        raise DmaError(rc, "dma_kv_read")
+    return k, v
+
+
+def dma_cache_attn(q: torch.Tensor, cache: KVCache, start: torch.Tensor, n_tokens: torch.Tensor | None = None, *, window: int = 0,
+                   sink_tokens: int = 0, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """q [B, Hq, N, D] bf16 (any strides with dense rows), token i of sequence b at position start[b] + i, attends to the
+    cache's keys at and before its own position (window > 0: to the last `window` of them and the first sink_tokens positions)
+    -> out [B, Hq, N, D] bf16.  Rows behind n_tokens are left as they were in out; without out they are zeros.
+    workspace: contiguous uint8 of at least dma_cache_attn_workspace_bytes(...) bytes, for one call at a time; by default one
+    is allocated."""
+    ps, pn = _spans(cache, start, n_tokens)
+    if q.dim() != 4:
+        raise ValueError("q must be [B, Hq, N, D]")
+    device = cache.device
+    _, Hq, N, _ = q.shape
+    shape = (cache.B, Hq, N, cache.D)
+    rq = _rows(q, "q", shape, device)
+    if out is None:
+        out = (torch.empty if n_tokens is None else torch.zeros)(shape, dtype=torch.bfloat16, device=device)
+    ro = _rows(out, "out", shape, device)
+    L = load()
+    if workspace is None:
+        need = L.dma_cache_attn_workspace_bytes(cache.B, Hq, cache.Hkv, N, cache.D)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif workspace.device != device:
+        raise ValueError("workspace: need it on the cache's GPU")
+    pw, nw = (None, 0) if workspace is None else (_dev(workspace, torch.uint8, "workspace"), workspace.numel())
+    rc = L.dma_cache_attn(cache._ref, rq, ro, cache.B, Hq, N, ps, pn, int(window), int(sink_tokens), pw, nw, _stream())
+    if rc:
+        raise DmaError(rc, "dma_cache_attn")
+    return out
+
+
+def dma_cache_attn_workspace_bytes(B: int, Hq: int, Hkv: int, N: int, D: int) -> int:
+    """Bytes of workspace of a dma_cache_attn call of these sizes on the current device."""
+    return int(load().dma_cache_attn_workspace_bytes(B, Hq, Hkv, N, D))
 
 
 def dma_diag_copy(src: torch.Tensor, dst: torch.Tensor) -> None:

@@ -20,6 +20,60 @@ int check_quant_common(const void* x, int64_t rows, int D)
     return DMA_OK;
 }
 
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// B == 0 or N == 0 is a no-op that never looks at the tensors' pointers (an empty tensor has none).
+int check_cache(const dma_kv_cache* cache, int B, int N, dma::CacheView& c)
+{
+    if (!cache || B < 0 || N < 0) return DMA_ERR_INVALID_ARG;
+    if (cache->fmt != DMA_FMT_MXFP8_E4M3 && cache->fmt != DMA_FMT_MXFP8_E5M2) return valid_fmt(cache->fmt) ? DMA_ERR_UNSUPPORTED : DMA_ERR_INVALID_ARG;
+    if (cache->num_pages < 0 || cache->max_pages < 0 || cache->page_tokens <= 0 || cache->Hkv <= 0 || cache->D <= 0) return DMA_ERR_INVALID_ARG;
+    const int P = cache->page_tokens;
+    if (P < 16 || P > 256 || (P & (P - 1)) != 0) return DMA_ERR_UNSUPPORTED;
+    if (cache->D != 64 && cache->D != 128) return DMA_ERR_UNSUPPORTED;
+    if ((int64_t)cache->max_pages * P >= (int64_t)1 << 30 || N >= 1 << 30) return DMA_ERR_UNSUPPORTED;
+    if (cache->num_pages > (((int64_t)1 << 40) - 1) / P / cache->D / cache->Hkv) return DMA_ERR_UNSUPPORTED;
+    if (B > 0 && N > 0) {
+        if (cache->num_pages > 0 && (!cache->k_codes || !cache->v_codes || !cache->k_scales || !cache->v_scales)) return DMA_ERR_INVALID_ARG;
+        if (cache->max_pages > 0 && !cache->page_table) return DMA_ERR_INVALID_ARG;
+        if (!aligned16(cache->k_codes) || !aligned16(cache->v_codes) || !aligned4(cache->page_table)) return DMA_ERR_INVALID_ARG;
+    }
+    c.k_codes = (uint8_t*)cache->k_codes; c.v_codes = (uint8_t*)cache->v_codes;
+    c.k_scales = (uint8_t*)cache->k_scales; c.v_scales = (uint8_t*)cache->v_scales;
+    c.page_table = (const int*)cache->page_table;
+    c.num_pages = cache->num_pages;
+    c.max_pages = cache->max_pages;
+    c.page_shift = __builtin_ctz((unsigned)P);
+    c.Hkv = cache->Hkv;
+    c.D = cache->D;
+    c.e5m2 = cache->fmt == DMA_FMT_MXFP8_E5M2;
+    return DMA_OK;
+}
+
+int check_spans(const void* start, const void* n_tokens, int B, int N, dma::Spans& s)
+{
+    if (!start || !aligned4(start) || !aligned4(n_tokens)) return DMA_ERR_INVALID_ARG;
+    s.start = (const int*)start; s.n_tokens = (const int*)n_tokens;
+    s.B = B; s.N = N;
+    return DMA_OK;
+}
+
+int check_rows(const dma_rows* r, dma::Rows& out)
+{
+    if (!r || !r->data || !aligned16(r->data)) return DMA_ERR_INVALID_ARG;
+    if (r->stride_batch < 0 || r->stride_head < 0 || r->stride_token < 0) return DMA_ERR_INVALID_ARG;
+    if (r->stride_batch % 8 != 0 || r->stride_head % 8 != 0 || r->stride_token % 8 != 0) return DMA_ERR_INVALID_ARG;
+    out.data = (char*)r->data;
+    out.stride_batch = 2 * r->stride_batch; out.stride_head = 2 * r->stride_head; out.stride_token = 2 * r->stride_token;
+    return DMA_OK;
+}
+
+// Query rows and work items of the attention over the cache are counted in 32 bits.
+bool attn_sizes_fit(int B, int Hq, int Hkv, int N)
+{
+    return (int64_t)N * (Hq / Hkv) <= 1 << 30 && (int64_t)B * Hq <= (1 << 30) / N;
+}
+
 }  // namespace
 
 static int quantize_one(const void* x_bf16, int64_t rows, int D, int fmt, int is_query, void* codes_u8,
@@ -152,6 +206,56 @@ int dma_attn_fwd(const void* q, const void* k, const void* v, void* out, int B, 
 
 size_t dma_attn_fwd_workspace_bytes(int, int, int, int, int) { return 0; }
 
+int dma_kv_write(const dma_kv_cache* cache, const dma_rows* k, const dma_rows* v, int B, int N, const void* start_i32,
+                 const void* n_tokens_i32, void* stream)
+{
+    dma::CacheView c;
+    dma::Spans s;
+    dma::Rows rk, rv;
+    int rc = check_cache(cache, B, N, c);
+    if (rc != DMA_OK || B == 0 || N == 0) return rc;
+    if ((rc = check_spans(start_i32, n_tokens_i32, B, N, s)) != DMA_OK) return rc;
+    if ((rc = check_rows(k, rk)) != DMA_OK || (rc = check_rows(v, rv)) != DMA_OK) return rc;
+    return dma::launch_kv_write(c, rk, rv, s, (hipStream_t)stream);
+}
+
+int dma_kv_read(const dma_kv_cache* cache, const dma_rows* k_out, const dma_rows* v_out, int B, int N, const void* start_i32,
+                const void* n_tokens_i32, void* stream)
+{
+    dma::CacheView c;
+    dma::Spans s;
+    dma::Rows rk, rv;
+    int rc = check_cache(cache, B, N, c);
+    if (rc != DMA_OK || B == 0 || N == 0) return rc;
+    if ((rc = check_spans(start_i32, n_tokens_i32, B, N, s)) != DMA_OK) return rc;
+    if ((rc = check_rows(k_out, rk)) != DMA_OK || (rc = check_rows(v_out, rv)) != DMA_OK) return rc;
+    return dma::launch_kv_read(c, rk, rv, s, (hipStream_t)stream);
+}
+
+int dma_cache_attn(const dma_kv_cache* cache, const dma_rows* q, const dma_rows* out, int B, int Hq, int N, const void* start_i32,
+                   const void* n_tokens_i32, int window, int sink_tokens, void* workspace, size_t workspace_bytes, void* stream)
+{
+    dma::CacheView c;
+    dma::Spans s;
+    dma::Rows rq, ro;
+    int rc = check_cache(cache, B, N, c);
+    if (rc != DMA_OK) return rc;
+    if (Hq <= 0 || Hq % c.Hkv != 0 || window < 0 || sink_tokens < 0) return DMA_ERR_INVALID_ARG;
+    if (B == 0 || N == 0) return DMA_OK;
+    if ((rc = check_spans(start_i32, n_tokens_i32, B, N, s)) != DMA_OK) return rc;
+    if ((rc = check_rows(q, rq)) != DMA_OK || (rc = check_rows(out, ro)) != DMA_OK) return rc;
+    if (!attn_sizes_fit(B, Hq, c.Hkv, N)) return DMA_ERR_UNSUPPORTED;
+    const size_t need = dma::cache_attn_workspace(B, Hq, c.Hkv, N, c.D);
+    if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return DMA_ERR_INVALID_ARG;
+    return dma::launch_cache_attn(c, rq, ro, s, Hq, window, sink_tokens, workspace, (hipStream_t)stream);
+}
+
+size_t dma_cache_attn_workspace_bytes(int B, int Hq, int Hkv, int N, int D)
+{
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || N <= 0 || Hq % Hkv != 0 || (D != 64 && D != 128) || !attn_sizes_fit(B, Hq, Hkv, N)) return 0;
+    return dma::cache_attn_workspace(B, Hq, Hkv, N, D);
+}
+
 int dma_diag_copy(const void* src, void* dst, int64_t bytes, void* stream)
 {
     if (bytes < 0 || bytes % 16 != 0) return DMA_ERR_INVALID_ARG;
@@ -193,6 +297,6 @@ const char* dma_error_string(int code)
     return "unknown error code";
 }
 
-int dma_version(void) { return 100; }
+int dma_version(void) { return 200; }
 
 }  // extern "C"

@@ -52,4 +52,33 @@ int launch_group_amax(const void* x, int64_t n_mat, int64_t S, int D, int is_que
 
 int launch_attn_fwd(const AttnArgs& a, hipStream_t stream);
 
+// The paged 8-bit key / value cache (sizes checked by the caller).
+struct CacheView {
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    uint8_t* k_scales;
+    uint8_t* v_scales;
+    const int* page_table;
+    int64_t num_pages;
+    int max_pages, page_shift, Hkv, D;
+    bool e5m2;
+};
+struct Rows {
+    char* data;
+    int64_t stride_batch, stride_head, stride_token;    // bytes
+};
+// Which tokens a call speaks of: positions [start[b], start[b] + n) with n = n_tokens[b] (clamped) or N.
+struct Spans {
+    const int* start;
+    const int* n_tokens;
+    int B, N;
+};
+
+int launch_kv_write(const CacheView& c, const Rows& k, const Rows& v, const Spans& s, hipStream_t stream);
+int launch_kv_read(const CacheView& c, const Rows& k, const Rows& v, const Spans& s, hipStream_t stream);
+
+int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const Spans& s, int Hq, int window, int sinks,
+                      void* workspace, hipStream_t stream);
+size_t cache_attn_workspace(int B, int Hq, int Hkv, int N, int D);
+
 }  // namespace dma
