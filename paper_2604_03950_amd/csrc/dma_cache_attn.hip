@@ -1,94 +1,621 @@
-// Attention over the paged 8-bit cache, the plain way: one wave per query row, 64 keys at a time, a lane per key for the scores
-// and a lane per channel (two at D = 128) for the values.  Online softmax in base 2, everything in binary32.
+// Attention over the paged 8-bit cache for few query rows per kv head (single tokens, drafts): bound by the bytes of the cache.
+//
+// Rows: the query tokens of a sequence times the G query heads of a kv head, token by token, in tiles of 16 * MT.  A step is 64
+// positions.  A wave forms S^T = K Q^T with the matrix instruction's 16 rows set to positions such that lane group g (16 lanes) of
+// the result holds positions 16 g .. 16 g + 15 of the step, 4 per product: exactly the ones whose probabilities that group has to
+// give to O^T = V^T P^T, so P never leaves its lane, and each operand of V is 16 consecutive bytes of the cache (its positions lie
+// innermost).  Codes go from memory to registers once and are decoded to bf16 there, times the page's scale (exact); no LDS until
+// the waves of a workgroup, which take turns at the steps, join their sums.
+//
+// Softmax: base 2, one maximum per row, raised only when a score exceeds it by 8 units (then everything is scaled down): p <= 2^8,
+// which neither binary32 sums nor bf16's rounding of p notice, and a step needs no exchange between lanes.
+//
+// Long and uneven sequences: the steps of all (sequence, kv head, row tile) items form one line that is cut into equal shares, one
+// per workgroup.  An item that lies in one share is written directly; pieces of the others go to the workspace, and a second
+// kernel joins them.
 #include "dma_device.hpp"
 #include "dma_internal.hpp"
+#include <algorithm>
+#include <atomic>
 #include <math.h>
 
 namespace dma {
 
-template <bool E5M2>
-DMA_DEV float decode1(unsigned byte, float sc)
+constexpr int STEP = 64;                     // positions of a step
+constexpr int POS_MAX = 1 << 30;             // above every position that a table holds
+constexpr float M_NONE = -3.0e38f;           // the maximum of nothing: below every score, and finite
+
+struct CacheAttnArgs {
+    CacheView c;
+    Rows q, out;
+    Spans s;
+    int G;                   // query heads per kv head
+    int row_tiles;           // of a sequence with N tokens
+    int window, sinks;
+    int capacity;            // positions that a reader may find
+    float scale;             // log2(e) / sqrt(D)
+    int min_share;
+    float* pieces;           // 2 per workgroup: [ROWS][D] sums, then [ROWS] maxima, then [ROWS] weights
+    int2* split;             // per item: first and last workgroup that has a piece (first = last: no pieces)
+};
+
+struct SeqInfo {
+    int start, n;
+};
+DMA_DEV SeqInfo seq_of(const CacheAttnArgs& a, int b)
 {
-    if constexpr (E5M2) return __builtin_amdgcn_cvt_scalef32_f32_bf8(byte, sc, 0);
-    else return __builtin_amdgcn_cvt_scalef32_f32_fp8(byte, sc, 0);
+    SeqInfo q;
+    q.start = a.s.start[b];
+    q.n = a.s.n_tokens ? min(max(a.s.n_tokens[b], 0), a.s.N) : a.s.N;
+    if (q.start < 0) q.n = 0;
+    return q;
 }
 
-template <int D, bool E5M2>
-__global__ void __launch_bounds__(64)
-cache_attn_row_kernel(CacheView c, Rows q, Rows out, Spans s, int Hq, int window, int sinks, float scale)
+// The steps that a row tile visits: [0, sink_steps) and [first, first + steps - sink_steps).
+struct StepRange {
+    int sink_steps, first, steps;
+    DMA_DEV int position(int j) const { return (j < sink_steps ? j : first + j - sink_steps) * STEP; }
+};
+template <int ROWS>
+DMA_DEV StepRange range_of(const CacheAttnArgs& a, const SeqInfo& q, int tile)
 {
-    const int lane = threadIdx.x;
-    unsigned r = blockIdx.x;
-    const int h = r % (unsigned)Hq;
-    r /= (unsigned)Hq;
-    const int i = r % (unsigned)s.N, b = r / (unsigned)s.N;
-    const int start = s.start[b], n = s.n_tokens ? min(max(s.n_tokens[b], 0), s.N) : s.N;
-    if (start < 0 || i >= n) return;
-    const int64_t at = (int64_t)start + i;
-    const int end = (int)min(at + 1, (int64_t)c.max_pages << c.page_shift);
-    const int64_t from = window ? at - window + 1 : 0;
-    const int kvh = h / (Hq / c.Hkv), P = 1 << c.page_shift;
-    __shared__ float qs[D], ps[64];
-    __shared__ int64_t slabs[64];
-    const unsigned short* qp = (const unsigned short*)(q.data + b * q.stride_batch + h * q.stride_head + i * q.stride_token);
-    for (int d = lane; d < D; d += 64) qs[d] = __int_as_float((int)qp[d] << 16);
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, o[D / 64] = {};
-    for (int t0 = 0; t0 < end; t0 += 64) {
-        const int t = t0 + lane;
-        int64_t slab = -1;
-        if (t < end && (t >= from || t < sinks)) {
-            const int page = c.page_table[(int64_t)b * c.max_pages + (t >> c.page_shift)];
-            if (page >= 0 && page < c.num_pages) slab = (int64_t)page * c.Hkv + kvh;
+    const int64_t from = (int64_t)q.start + tile * ROWS / a.G, to = (int64_t)q.start + min(q.n - 1, (tile * ROWS + ROWS - 1) / a.G);
+    const int hi = (int)min(to + 1, (int64_t)a.capacity);
+    const int lo = a.window ? (int)min(max(from - a.window + 1, (int64_t)0), (int64_t)hi) : 0;
+    StepRange r;
+    r.first = lo / STEP;
+    r.sink_steps = (min(a.sinks, hi) + STEP - 1) / STEP;
+    if (r.sink_steps >= r.first) r.sink_steps = r.first = 0;
+    r.steps = r.sink_steps + (hi + STEP - 1) / STEP - r.first;
+    return r;
+}
+
+template <bool E5M2, bool HI>
+DMA_DEV int decode2(int w, float sc)
+{
+    if constexpr (E5M2) return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((unsigned)w, sc, HI));
+    else return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w, sc, HI));
+}
+// Eight codes -> eight bf16, an operand of the matrix instruction.
+template <bool E5M2>
+DMA_DEV v8bf decode8(int lo, int hi, float sc)
+{
+    v4i r;
+    r[0] = decode2<E5M2, false>(lo, sc);
+    r[1] = decode2<E5M2, true>(lo, sc);
+    r[2] = decode2<E5M2, false>(hi, sc);
+    r[3] = decode2<E5M2, true>(hi, sc);
+    return __builtin_bit_cast(v8bf, r);
+}
+DMA_DEV float cross_group_max(float x) { return cross_half_max(row_pair_max(x)); }
+DMA_DEV float cross_group_sum(float x)
+{
+    const v2u r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return cross_half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+DMA_DEV int pack_bf16(float a, float b)
+{
+    v2bf r;
+    r[0] = (__bf16)a;
+    r[1] = (__bf16)b;
+    return __builtin_bit_cast(int, r);
+}
+
+// Bytes that are no number (NaN, infinity): bit 7 of each.
+template <bool E5M2>
+DMA_DEV unsigned no_number(unsigned w) { return ((w & 0x7f7f7f7fu) + (E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u; }
+
+// BY_ITEM: one workgroup per item.  Otherwise the items' steps in equal shares.
+template <int D, bool E5M2, int MT, int W, bool BY_ITEM>
+__global__ void __launch_bounds__(64 * W, MT == 1 ? (W == 4 ? 3 : 2) : 2)
+cache_attn_kernel(CacheAttnArgs a)
+{
+    constexpr int ROWS = 16 * MT, KJ = D / 64, DT = D / 16, LD = D + 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+    __shared__ float obuf[W / 2][ROWS][LD];
+    __shared__ float ml[W / 2][2][ROWS];
+    __shared__ int64_t scan[W + 1];
+    const CacheView& c = a.c;
+    const int page_mask = (1 << c.page_shift) - 1;
+
+    // ---- where this workgroup's share lies
+    int64_t begin = 0, left = 1;             // in steps; of the line
+    int b = 0, h = 0, tile = 0;
+    SeqInfo sq;
+    int skip = 0;                            // steps of the first item that belong to others
+    int wg = 0;                              // place in the line
+    if constexpr (BY_ITEM) {
+        unsigned i = blockIdx.x;
+        tile = i % (unsigned)a.row_tiles;
+        i /= (unsigned)a.row_tiles;
+        h = i % (unsigned)c.Hkv;
+        b = i / (unsigned)c.Hkv;
+        sq = seq_of(a, b);
+        if ((int64_t)tile * ROWS >= (int64_t)sq.n * a.G) return;
+    } else {
+        auto weight = [&](int bb) -> int64_t {                    // of one kv head of a sequence
+            if (bb >= a.s.B) return 0;
+            const SeqInfo q = seq_of(a, bb);
+            const int tiles = (int)(((int64_t)q.n * a.G + ROWS - 1) / ROWS);
+            int64_t t = 0;
+            for (int i = 0; i < tiles; ++i) t += max(range_of<ROWS>(a, q, i).steps, 1);
+            return t * c.Hkv;
+        };
+        auto inclusive = [&](int64_t x) {                         // over the workgroup; the total goes to scan[W]
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int64_t y = __shfl_up(x, o);
+                if (lane >= o) x += y;
+            }
+            __syncthreads();
+            if (lane == 63) scan[wave] = x;
+            __syncthreads();
+            int64_t before = 0, all = 0;
+            for (int w = 0; w < W; ++w) {
+                if (w < wave) before += scan[w];
+                all += scan[w];
+            }
+            if (threadIdx.x == 0) scan[W] = all;
+            __syncthreads();
+            return x + before;
+        };
+        int64_t total = 0, mine = 0, upto = 0;
+        const int chunks = (a.s.B + 64 * W - 1) / (64 * W);
+        for (int k = 0; k < chunks; ++k) {
+            mine = weight(k * 64 * W + threadIdx.x);
+            upto = inclusive(mine);
+            total += scan[W];
         }
-        float x = -INFINITY;
-        if (slab >= 0) {
-            const uint8_t* row = c.k_codes + ((slab << c.page_shift) + (t & (P - 1))) * D;
-            const float sc = __int_as_float((int)c.k_scales[slab] << 23);
-            x = 0.f;
-            for (int d = 0; d < D; ++d) x = fmaf(qs[d], decode1<E5M2>(row[d], sc), x);
-            x *= scale;
+        const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)a.min_share);
+        // workgroups next to each other in the line on the same XCD (they are dealt out in turn): they may share a sequence's keys
+        const int shares = (int)((total + share - 1) / share), per = (shares + 7) / 8;
+        if ((int)(blockIdx.x / 8) >= per) return;
+        wg = blockIdx.x % 8 * per + blockIdx.x / 8;
+        begin = share * wg;
+        if (begin >= total) return;
+        left = min(share, total - begin);
+        // the sequence that holds `begin`
+        __shared__ int found;
+        __shared__ int64_t found_at;
+        int64_t base = 0;
+        for (int k = 0; k < chunks; ++k) {
+            if (chunks > 1) {
+                mine = weight(k * 64 * W + threadIdx.x);
+                upto = inclusive(mine);
+            }
+            if (begin >= base + upto - mine && begin < base + upto) {
+                found = k * 64 * W + threadIdx.x;
+                found_at = begin - (base + upto - mine);
+            }
+            base += scan[W];
+            if (begin < base) break;
         }
-        float mx = x;
-        for (int w = 32; w; w >>= 1) mx = fmaxf(mx, __shfl_xor(mx, w));
-        if (mx == -INFINITY) continue;                            // nothing visible, the same for all lanes
-        mx = fmaxf(mx, m);
-        const float p = exp2f(x - mx), keep = exp2f(m - mx);
-        m = mx;
-        float sum = p;
-        for (int w = 32; w; w >>= 1) sum += __shfl_xor(sum, w);
-        l = l * keep + sum;
         __syncthreads();
-        ps[lane] = p;
-        slabs[lane] = slab;
-        __syncthreads();
-        for (int u = 0; u < D / 64; ++u) {
-            o[u] *= keep;
-            const int d = lane + 64 * u;
-            for (int k = 0; k < 64; ++k) {
-                const int64_t sl = slabs[k];
-                if (sl < 0) continue;
-                const float sc = __int_as_float((int)c.v_scales[sl] << 23);
-                o[u] = fmaf(ps[k], decode1<E5M2>(c.v_codes[((sl * D + d) << c.page_shift) + ((t0 + k) & (P - 1))], sc), o[u]);
+        b = found;
+        sq = seq_of(a, b);
+        const int tiles = (int)(((int64_t)sq.n * a.G + ROWS - 1) / ROWS);
+        int64_t per_head = 0;
+        for (int i = 0; i < tiles; ++i) per_head += max(range_of<ROWS>(a, sq, i).steps, 1);
+        int64_t at = found_at;
+        h = (int)(at / per_head);
+        at -= h * per_head;
+        for (;; ++tile) {
+            const int w = max(range_of<ROWS>(a, sq, tile).steps, 1);
+            if (at < w) break;
+            at -= w;
+        }
+        skip = (int)at;
+    }
+
+    // ---- item after item
+    for (;;) {
+        const StepRange range = range_of<ROWS>(a, sq, tile);
+        const int weight = max(range.steps, 1);
+        const int until = BY_ITEM ? weight : (int)min((int64_t)weight, skip + left);
+        const int rows = (int)min((int64_t)sq.n * a.G - tile * ROWS, (int64_t)ROWS);
+        const int from = sq.start;
+
+        // the query rows of this lane's column, and what they see: positions [vis_lo, vis_hi] and those below sinks
+        v8bf qf[MT][2 * KJ];
+        int vis_lo[MT], vis_hi[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = r / a.G;
+            const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + r - i * a.G) * a.q.stride_head + i * a.q.stride_token;
+#pragma unroll
+            for (int j = 0; j < KJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) qf[mt][2 * j + e] = *(const v8bf*)(qp + (j * 64 + grp * 16 + e * 8) * 2);
+            const int64_t p = (int64_t)from + i;
+            vis_hi[mt] = (int)min(p, (int64_t)POS_MAX);
+            vis_lo[mt] = a.window ? (int)min(max(p - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
+        }
+        // ... and what all of them see
+        const int all_hi = (int)min((int64_t)from + tile * ROWS / a.G, (int64_t)POS_MAX);
+        const int all_lo = a.window ? (int)min(max((int64_t)from + (tile * ROWS + rows - 1) / a.G - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
+
+        v4f o[MT][DT];
+        float m[MT], l[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[mt][dt] = v4f{0.f, 0.f, 0.f, 0.f};
+            m[mt] = M_NONE;
+            l[mt] = 0.f;
+        }
+
+        // Pages of a step: of the 16 positions whose keys this lane loads, and of those whose values it loads.
+        const int* table = c.page_table + (int64_t)b * c.max_pages;
+        auto page_of = [&](int j, int g) -> int {
+            const int pi = (range.position(j) + 16 * g) >> c.page_shift;
+            return pi < c.max_pages ? table[pi] : -1;
+        };
+        auto slab_of = [&](int page) -> int64_t { return (int64_t)((page >= 0 && page < c.num_pages) ? page : 0) * c.Hkv + h; };
+        v4i kr[4][KJ], vr[DT];
+        int k_scale, v_scale, v_page;
+        auto load_k = [&](int j, int page) {
+            const int64_t slab = slab_of(page);
+            const int place = ((range.position(j) + 16 * (col >> 2)) & page_mask) + (col & 3);
+            const uint8_t* p = c.k_codes + (((slab << c.page_shift) + place) * D + grp * 16);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int jj = 0; jj < KJ; ++jj) kr[t][jj] = *(const v4i*)(p + t * 4 * D + jj * 64);
+            k_scale = c.k_scales[slab];
+        };
+        auto load_v = [&](int j, int page) {
+            const int64_t slab = slab_of(page);
+            const int place = (range.position(j) + 16 * grp) & page_mask;
+            const uint8_t* p = c.v_codes + (((slab * D + col) << c.page_shift) + place);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) vr[dt] = *(const v4i*)(p + ((dt * 16) << c.page_shift));
+            v_scale = c.v_scales[slab];
+            v_page = page;
+        };
+
+        const int last = min(until, range.steps);
+        int j = skip + wave;
+        int pk = -1, pv = -1;                                     // pages of the step after the next
+        if (j < last) {
+            load_k(j, page_of(j, col >> 2));
+            load_v(j, page_of(j, grp));
+            if (j + W < last) {
+                pk = page_of(j + W, col >> 2);
+                pv = page_of(j + W, grp);
+            }
+        }
+        for (; j < last; j += W) {
+            const int pos = range.position(j);
+            const bool page_ok = v_page >= 0 && v_page < c.num_pages;
+            // ---- scores
+            v4f s[MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) s[mt][t] = v4f{0.f, 0.f, 0.f, 0.f};
+            const float ksc = __int_as_float(k_scale << 23);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int jj = 0; jj < KJ; ++jj)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const v8bf k = decode8<E5M2>(kr[t][jj][2 * e], kr[t][jj][2 * e + 1], ksc);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) s[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[mt][2 * jj + e], s[mt][t], 0, 0, 0);
+                    }
+            // ---- the next step's keys, the pages of the one after it
+            const int page_v = pv;
+            if (j + W < last) {
+                load_k(j + W, pk);
+                if (j + 2 * W < last) {
+                    pk = page_of(j + 2 * W, col >> 2);
+                    pv = page_of(j + 2 * W, grp);
+                }
+            }
+            // ---- what is not seen
+            const bool plain = pos + STEP - 1 <= all_hi && (pos >= all_lo || pos + STEP <= a.sinks) && __all(page_ok);
+            float x[MT][16];                                      // position 16 grp + 4 t + r of the step at 4 t + r
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[mt][e] = s[mt][e >> 2][e & 3];
+            if (!plain) {
+                unsigned seen[MT], any = 0;                       // bit e: the lane's 16 positions
+                const int base = pos + 16 * grp;
+                auto below = [&](int at) { return (1u << min(max(at - base, 0), 16)) - 1u; };
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    seen[mt] = page_ok ? below(vis_hi[mt] + 1) & (~below(vis_lo[mt]) | below(a.sinks)) : 0u;
+                    any |= seen[mt];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[mt][e] = (seen[mt] >> e) & 1u ? x[mt][e] : -INFINITY;
+                }
+                // over the rows: 16 columns hold different rows of the same positions
+                any |= __builtin_amdgcn_mov_dpp(any, 0x121, 0xF, 0xF, true);
+                any |= __builtin_amdgcn_mov_dpp(any, 0x122, 0xF, 0xF, true);
+                any |= __builtin_amdgcn_mov_dpp(any, 0x124, 0xF, 0xF, true);
+                any |= __builtin_amdgcn_mov_dpp(any, 0x128, 0xF, 0xF, true);
+                // values that no row sees may be anything: zeros instead
+                unsigned bad = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const unsigned nib = (any >> (4 * w)) & 15u;
+                    const unsigned keep = ((nib & 1) ? 0xffu : 0) | ((nib & 2) ? 0xff00u : 0) | ((nib & 4) ? 0xff0000u : 0) | ((nib & 8) ? 0xff000000u : 0);
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        vr[dt][w] &= (int)keep;
+                        bad |= no_number<E5M2>((unsigned)vr[dt][w]);
+                    }
+                }
+                // a NaN that some rows see and some do not must not reach the others through a probability of zero: it is
+                // taken out of the product, and the sums of the rows that see it (counted by a product of their own) become NaN
+                if (__any(bad != 0)) {
+                    // two flags (bits 0 and SHIFT) -> two bf16, 0 or 1
+                    auto ones = [](unsigned f, int shift) { return (int)((f & 1u) * 0x3f80u | ((f >> shift) & 1u) * 0x3f800000u); };
+                    v8bf sf[MT][2];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const unsigned f = seen[mt] >> (8 * e);
+                            sf[mt][e] = __builtin_bit_cast(v8bf, v4i{ones(f, 1), ones(f >> 2, 1), ones(f >> 4, 1), ones(f >> 6, 1)});
+                        }
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        unsigned f[4];
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            f[w] = no_number<E5M2>((unsigned)vr[dt][w]) >> 7;
+                            vr[dt][w] &= (int)~(f[w] * 0xffu);
+                        }
+                        v8bf nf[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            nf[e] = __builtin_bit_cast(v8bf, v4i{ones(f[2 * e], 8), ones(f[2 * e] >> 16, 8), ones(f[2 * e + 1], 8), ones(f[2 * e + 1] >> 16, 8)});
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            v4f count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[0], sf[mt][0], v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                            count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[1], sf[mt][1], count, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (count[r] > 0.f) o[mt][dt][r] = NAN;
+                        }
+                    }
+                }
+            }
+            // ---- softmax
+            v8bf pf[MT][2];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                float top = x[mt][0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) top = fmaxf(top, x[mt][e]);
+                if (__any((top - m[mt]) * a.scale > 8.f)) {
+                    const float up = fmaxf(m[mt], cross_group_max(top)), down = __builtin_amdgcn_exp2f((m[mt] - up) * a.scale);
+                    m[mt] = up;
+                    l[mt] *= down;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) o[mt][dt] *= down;
+                }
+                const float off = m[mt] * a.scale;
+                int pw[8];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(x[mt][e], a.scale, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(x[mt][e + 1], a.scale, -off));
+                    l[mt] += p0 + p1;
+                    pw[e / 2] = pack_bf16(p0, p1);
+                }
+                pf[mt][0] = __builtin_bit_cast(v8bf, v4i{pw[0], pw[1], pw[2], pw[3]});
+                pf[mt][1] = __builtin_bit_cast(v8bf, v4i{pw[4], pw[5], pw[6], pw[7]});
+            }
+            // ---- values
+            const float vsc = __int_as_float(v_scale << 23);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const v8bf v = decode8<E5M2>(vr[dt][2 * e], vr[dt][2 * e + 1], vsc);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[mt][e], o[mt][dt], 0, 0, 0);
+                }
+            if (j + W < last) load_v(j + W, page_v);
+        }
+
+        // ---- the waves' sums, half of them at a time
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) l[mt] = cross_group_sum(l[mt]);
+#pragma unroll
+        for (int half = W / 2; half; half >>= 1) {
+            if (wave >= half && wave < 2 * half) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) *(v4f*)&obuf[wave - half][mt * 16 + col][dt * 16 + grp * 4] = o[mt][dt];
+                    if (grp == 0) {
+                        ml[wave - half][0][mt * 16 + col] = m[mt];
+                        ml[wave - half][1][mt * 16 + col] = l[mt];
+                    }
+                }
+            }
+            __syncthreads();
+            if (wave < half) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const float m2 = ml[wave][0][mt * 16 + col], up = fmaxf(m[mt], m2);
+                    const float f1 = __builtin_amdgcn_exp2f((m[mt] - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2 - up) * a.scale);
+                    m[mt] = up;
+                    l[mt] = l[mt] * f1 + ml[wave][1][mt * 16 + col] * f2;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const v4f x = *(const v4f*)&obuf[wave][mt * 16 + col][dt * 16 + grp * 4];
+                        o[mt][dt] = o[mt][dt] * f1 + x * f2;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        const bool whole = BY_ITEM || (skip == 0 && until == weight);
+        if (wave == 0) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const int rr = mt * 16 + col;
+                if (rr >= rows) continue;
+                if (whole) {
+                    const int r = tile * ROWS + rr, i = r / a.G;
+                    char* op = a.out.data + b * a.out.stride_batch + (h * a.G + r - i * a.G) * a.out.stride_head + i * a.out.stride_token;
+                    const float inv = l[mt] == 0.f ? 0.f : 1.f / l[mt];
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const v4f x = o[mt][dt] * inv;
+                        *(v2i*)(op + (dt * 16 + grp * 4) * 2) = v2i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+                    }
+                } else {
+                    float* p = a.pieces + (int64_t)(2 * wg + (skip == 0)) * (ROWS * (D + 2));
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) *(v4f*)(p + rr * D + dt * 16 + grp * 4) = o[mt][dt];
+                    if (grp == 0) {
+                        p[ROWS * D + rr] = m[mt];
+                        p[ROWS * D + ROWS + rr] = l[mt];
+                    }
+                }
+            }
+            if (!BY_ITEM && lane == 0) {
+                int* sp = (int*)(a.split + ((int64_t)b * c.Hkv + h) * a.row_tiles + tile);
+                if (skip == 0) sp[0] = wg;                         // the first piece's workgroup says so ...
+                if (until == weight) sp[1] = wg;                   // ... and the last one's
+            }
+        }
+        if constexpr (BY_ITEM) return;
+        else {
+            left -= until - skip;
+            if (left <= 0) return;
+            skip = 0;
+            ++tile;
+            while ((int64_t)tile * ROWS >= (int64_t)sq.n * a.G) {
+                tile = 0;
+                if (h + 1 < c.Hkv && sq.n > 0) ++h;
+                else {
+                    h = 0;
+                    sq = seq_of(a, ++b);
+                }
             }
         }
     }
-    __bf16* op = (__bf16*)(out.data + b * out.stride_batch + h * out.stride_head + i * out.stride_token);
-    for (int u = 0; u < D / 64; ++u) op[lane + 64 * u] = (__bf16)(l > 0.f ? o[u] / l : 0.f);
+}
+
+// Joins the pieces of split items: a workgroup per item and 4 of its rows; threads over channels (4 each), rows and pieces.
+template <int D, int ROWS>
+__global__ void __launch_bounds__(512)
+cache_attn_join_kernel(CacheAttnArgs a)
+{
+    constexpr int CH = D / 4, PG = 512 / (4 * CH);
+    unsigned item = blockIdx.x;
+    const int tile = item % (unsigned)a.row_tiles;
+    const int h = item / (unsigned)a.row_tiles % (unsigned)a.c.Hkv, b = item / (unsigned)a.row_tiles / (unsigned)a.c.Hkv;
+    const SeqInfo sq = seq_of(a, b);
+    const int rows = (int)min((int64_t)sq.n * a.G - tile * ROWS, (int64_t)ROWS);
+    const int rr = blockIdx.y * 4 + threadIdx.x / CH % 4, ch = threadIdx.x % CH, pg = threadIdx.x / (4 * CH);
+    if ((int)blockIdx.y * 4 >= rows) return;
+    const int2 sp = a.split[item];
+    if (sp.x == sp.y) return;
+    __shared__ v4f os[PG][4][CH];
+    __shared__ float ms[PG][4], ls[PG][4];
+    v4f o = {0.f, 0.f, 0.f, 0.f};
+    float m = M_NONE, l = 0.f;
+    if (rr < rows) {
+        for (int w = sp.x + pg; w <= sp.y; w += PG) {
+            const float* p = a.pieces + (int64_t)(2 * w + (w == sp.x)) * (ROWS * (D + 2));
+            const float m2 = p[ROWS * D + rr], l2 = p[ROWS * D + ROWS + rr], up = fmaxf(m, m2);
+            const v4f x = *(const v4f*)(p + rr * D + ch * 4);
+            const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2 - up) * a.scale);
+            m = up;
+            l = l * f1 + l2 * f2;
+            o = o * f1 + x * f2;
+        }
+    }
+    os[pg][rr & 3][ch] = o;
+    if (ch == 0) {
+        ms[pg][rr & 3] = m;
+        ls[pg][rr & 3] = l;
+    }
+    __syncthreads();
+    if (pg || rr >= rows) return;
+    for (int k = 1; k < PG; ++k) {
+        const float m2 = ms[k][rr & 3], up = fmaxf(m, m2);
+        const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2 - up) * a.scale);
+        m = up;
+        l = l * f1 + ls[k][rr & 3] * f2;
+        o = o * f1 + os[k][rr & 3][ch] * f2;
+    }
+    const int r = tile * ROWS + rr, i = r / a.G;
+    char* op = a.out.data + b * a.out.stride_batch + (h * a.G + r - i * a.G) * a.out.stride_head + i * a.out.stride_token;
+    const v4f x = o * (l == 0.f ? 0.f : 1.f / l);
+    *(v2i*)(op + ch * 8) = v2i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+}
+
+// ---------------------------------------------------------------------------------------------------------------- host
+static int cache_cus()
+{
+    static std::atomic<int> cached[64];
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+    n = cached[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) return 256;
+        cached[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+// Rows per workgroup: 16 where a kv head has no more, else 32.
+static int mt_of(int G, int N) { return (int64_t)G * N <= 16 ? 1 : 2; }
+static int64_t grid_of(int mt) { return (int64_t)cache_cus() * (mt == 1 ? 3 : 2); }
+
+size_t cache_attn_workspace(int B, int Hq, int Hkv, int N, int D)
+{
+    const int mt = mt_of(Hq / Hkv, N);
+    const int64_t tiles = ((int64_t)N * (Hq / Hkv) + 16 * mt - 1) / (16 * mt), items = (int64_t)B * Hkv * tiles;
+    return (size_t)(2 * grid_of(mt) * (16 * mt) * (D + 2) * 4 + items * 8);
+}
+
+template <int D, bool E5M2, int MT>
+static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
+{
+    constexpr int ROWS = 16 * MT;
+    const int64_t tiles = ((int64_t)a.s.N * a.G + ROWS - 1) / ROWS, items = (int64_t)a.s.B * a.c.Hkv * tiles;
+    if (items * 512 > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
+    a.row_tiles = (int)tiles;
+    a.min_share = 8;
+    // the most steps that an item can have
+    const int64_t reach = a.window ? std::min((int64_t)a.capacity, (int64_t)a.window + a.sinks + ROWS / a.G + 3 * STEP) : a.capacity;
+    if (reach <= 20 * STEP)
+        return launch(cache_attn_kernel<D, E5M2, MT, 8, true>, dim3((unsigned)items), dim3(512), stream, a);
+    const int64_t grid = grid_of(MT);
+    a.pieces = (float*)workspace;
+    a.split = (int2*)(a.pieces + 2 * grid * ROWS * (D + 2));
+    const int rc = launch(cache_attn_kernel<D, E5M2, MT, 4, false>, dim3((unsigned)grid), dim3(256), stream, a);
+    if (rc != DMA_OK_) return rc;
+    return launch(cache_attn_join_kernel<D, ROWS>, dim3((unsigned)items, ROWS / 4), dim3(512), stream, a);
 }
 
 int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const Spans& s, int Hq, int window, int sinks,
-                      void*, hipStream_t stream)
+                      void* workspace, hipStream_t stream)
 {
-    using F = void(CacheView, Rows, Rows, Spans, int, int, int, float);
-    F* const kernels[2][2] = {{cache_attn_row_kernel<64, false>, cache_attn_row_kernel<64, true>},
-                              {cache_attn_row_kernel<128, false>, cache_attn_row_kernel<128, true>}};
-    const int64_t blocks = (int64_t)s.B * Hq * s.N;
-    if (blocks * 64 > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
-    return launch(kernels[c.D == 128][c.e5m2], dim3((unsigned)blocks), dim3(64), stream, c, q, out, s, Hq, window, window ? sinks : 0,
-                  (float)(1.4426950408889634074 / sqrt((double)c.D)));
+    CacheAttnArgs a = {};
+    a.c = c;
+    a.q = q;
+    a.out = out;
+    a.s = s;
+    a.G = Hq / c.Hkv;
+    a.window = window;
+    a.sinks = window ? sinks : 0;
+    a.capacity = c.num_pages ? c.max_pages << c.page_shift : 0;
+    a.scale = (float)(1.4426950408889634074 / sqrt((double)c.D));
+    const int mt = mt_of(a.G, s.N);
+    auto pick = [&](auto D, auto F) { return mt == 1 ? launch_few<D, F != 0, 1>(a, workspace, stream) : launch_few<D, F != 0, 2>(a, workspace, stream); };
+    if (c.D == 128) return c.e5m2 ? pick(IC<128>{}, IC<1>{}) : pick(IC<128>{}, IC<0>{});
+    return c.e5m2 ? pick(IC<64>{}, IC<1>{}) : pick(IC<64>{}, IC<0>{});
 }
-
-size_t cache_attn_workspace(int, int, int, int, int) { return 0; }
 
 }  // namespace dma
