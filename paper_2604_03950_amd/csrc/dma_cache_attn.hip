@@ -105,9 +105,12 @@ DMA_DEV int pack_bf16(float a, float b)
 template <bool E5M2>
 DMA_DEV unsigned no_number(unsigned w) { return ((w & 0x7f7f7f7fu) + (E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u; }
 
+// Bits 0 to 3 -> the four bytes of a dword.
+DMA_DEV int bytes_of(unsigned bits) { return (int)((((bits & 15u) * 0x00204081u) & 0x01010101u) * 0xffu); }
+
 // BY_ITEM: one workgroup per item.  Otherwise the items' steps in equal shares.
 template <int D, bool E5M2, int MT, int W, bool BY_ITEM>
-__global__ void __launch_bounds__(64 * W, MT == 1 ? (W == 4 ? 3 : 2) : 2)
+__global__ void __launch_bounds__(64 * W, 2)
 cache_attn_kernel(CacheAttnArgs a)
 {
     constexpr int ROWS = 16 * MT, KJ = D / 64, DT = D / 16, LD = D + 4;
@@ -320,8 +323,10 @@ cache_attn_kernel(CacheAttnArgs a)
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[mt][e] = s[mt][e >> 2][e & 3];
+            unsigned seen[MT];                                    // bit e: the lane's 16 positions
+            bool nan_seen = false;                                // some value that a row sees is no number
             if (!plain) {
-                unsigned seen[MT], any = 0;                       // bit e: the lane's 16 positions
+                unsigned any = 0;
                 const int base = pos + 16 * grp;
                 auto below = [&](int at) { return (1u << min(max(at - base, 0), 16)) - 1u; };
 #pragma unroll
@@ -340,49 +345,14 @@ cache_attn_kernel(CacheAttnArgs a)
                 unsigned bad = 0;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const unsigned nib = (any >> (4 * w)) & 15u;
-                    const unsigned keep = ((nib & 1) ? 0xffu : 0) | ((nib & 2) ? 0xff00u : 0) | ((nib & 4) ? 0xff0000u : 0) | ((nib & 8) ? 0xff000000u : 0);
+                    const int keep = bytes_of(any >> (4 * w));
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
-                        vr[dt][w] &= (int)keep;
+                        vr[dt][w] &= keep;
                         bad |= no_number<E5M2>((unsigned)vr[dt][w]);
                     }
                 }
-                // a NaN that some rows see and some do not must not reach the others through a probability of zero: it is
-                // taken out of the product, and the sums of the rows that see it (counted by a product of their own) become NaN
-                if (__any(bad != 0)) {
-                    // two flags (bits 0 and SHIFT) -> two bf16, 0 or 1
-                    auto ones = [](unsigned f, int shift) { return (int)((f & 1u) * 0x3f80u | ((f >> shift) & 1u) * 0x3f800000u); };
-                    v8bf sf[MT][2];
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const unsigned f = seen[mt] >> (8 * e);
-                            sf[mt][e] = __builtin_bit_cast(v8bf, v4i{ones(f, 1), ones(f >> 2, 1), ones(f >> 4, 1), ones(f >> 6, 1)});
-                        }
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        unsigned f[4];
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            f[w] = no_number<E5M2>((unsigned)vr[dt][w]) >> 7;
-                            vr[dt][w] &= (int)~(f[w] * 0xffu);
-                        }
-                        v8bf nf[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            nf[e] = __builtin_bit_cast(v8bf, v4i{ones(f[2 * e], 8), ones(f[2 * e] >> 16, 8), ones(f[2 * e + 1], 8), ones(f[2 * e + 1] >> 16, 8)});
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            v4f count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[0], sf[mt][0], v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                            count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[1], sf[mt][1], count, 0, 0, 0);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (count[r] > 0.f) o[mt][dt][r] = NAN;
-                        }
-                    }
-                }
+                nan_seen = __any(bad != 0);
             }
             // ---- softmax
             v8bf pf[MT][2];
@@ -411,14 +381,36 @@ cache_attn_kernel(CacheAttnArgs a)
             }
             // ---- values
             const float vsc = __int_as_float(v_scale << 23);
+            if (!nan_seen) {
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const v8bf v = decode8<E5M2>(vr[dt][2 * e], vr[dt][2 * e + 1], vsc);
+                    for (int e = 0; e < 2; ++e) {
+                        const v8bf v = decode8<E5M2>(vr[dt][2 * e], vr[dt][2 * e + 1], vsc);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[mt][e], o[mt][dt], 0, 0, 0);
-                }
+                        for (int mt = 0; mt < MT; ++mt) o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[mt][e], o[mt][dt], 0, 0, 0);
+                    }
+            } else {
+                // It must not reach the rows that do not see it through a probability of zero: row after row, with what the row
+                // does not see taken out.  (A step that all rows see in full has no such rows.)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll 1
+                    for (int row = 0; row < 16; ++row) {
+                        const unsigned mine = (unsigned)__shfl((int)seen[mt], (lane & 48) + row);
+                        const int keep[4] = {bytes_of(mine), bytes_of(mine >> 4), bytes_of(mine >> 8), bytes_of(mine >> 12)};
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) {
+                            v4f x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                    decode8<E5M2>(vr[dt][2 * e] & keep[2 * e], vr[dt][2 * e + 1] & keep[2 * e + 1], vsc), pf[mt][e], x, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) o[mt][dt][r] += col == row ? x[r] : 0.f;
+                        }
+                    }
+            }
             if (j + W < last) load_v(j + W, page_v);
         }
 
@@ -570,7 +562,7 @@ static int cache_cus()
 
 // Rows per workgroup: 16 where a kv head has no more, else 32.
 static int mt_of(int G, int N) { return (int64_t)G * N <= 16 ? 1 : 2; }
-static int64_t grid_of(int mt) { return (int64_t)cache_cus() * (mt == 1 ? 3 : 2); }
+static int64_t grid_of(int mt) { return (int64_t)cache_cus() * 2; }
 
 size_t cache_attn_workspace(int B, int Hq, int Hkv, int N, int D)
 {
