@@ -4,8 +4,7 @@
 // chunks of 8 elements (16 bytes).  For keys, consecutive threads have consecutive chunks; for values a thread's four chunks
 // are the same 8 channels of four consecutive positions, so that the codes of a channel leave as whole dwords (positions lie
 // innermost), 16 threads covering 64 consecutive bytes and 4 of them 64 bytes of a row on the other side.
-#include "dma_device.hpp"
-#include "dma_internal.hpp"
+#include "dma_cache_device.hpp"
 #include <algorithm>
 
 namespace dma {
@@ -227,14 +226,6 @@ kv_write_kernel(CacheView c, Rows k, Rows v, Spans s, int pages_per_seq)
             }
         }
     }
-}
-
-// Two codes (the lower or upper half of a dword) -> two bf16, times 2^(scale - 127): exact.
-template <bool E5M2, bool HI>
-DMA_DEV int decode2(unsigned w, float sc)
-{
-    if constexpr (E5M2) return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, sc, HI));
-    else return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, sc, HI));
 }
 
 template <int D, bool E5M2>

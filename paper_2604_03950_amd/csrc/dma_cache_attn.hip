@@ -13,100 +13,14 @@
 // Long and uneven sequences: the steps of all (sequence, kv head, row tile) items form one line that is cut into equal shares, one
 // per workgroup.  An item that lies in one share is written directly; pieces of the others go to the workspace, and a second
 // kernel joins them.
-#include "dma_device.hpp"
-#include "dma_internal.hpp"
+#include "dma_cache_device.hpp"
 #include <algorithm>
 #include <atomic>
 #include <math.h>
 
 namespace dma {
 
-constexpr int STEP = 64;                     // positions of a step
-constexpr int POS_MAX = 1 << 30;             // above every position that a table holds
-constexpr float M_NONE = -3.0e38f;           // the maximum of nothing: below every score, and finite
-
-struct CacheAttnArgs {
-    CacheView c;
-    Rows q, out;
-    Spans s;
-    int G;                   // query heads per kv head
-    int row_tiles;           // of a sequence with N tokens
-    int window, sinks;
-    int capacity;            // positions that a reader may find
-    float scale;             // log2(e) / sqrt(D)
-    int min_share;
-    float* pieces;           // 2 per workgroup: [ROWS][D] sums, then [ROWS] maxima, then [ROWS] weights
-    int2* split;             // per item: first and last workgroup that has a piece (first = last: no pieces)
-};
-
-struct SeqInfo {
-    int start, n;
-};
-DMA_DEV SeqInfo seq_of(const CacheAttnArgs& a, int b)
-{
-    SeqInfo q;
-    q.start = a.s.start[b];
-    q.n = a.s.n_tokens ? min(max(a.s.n_tokens[b], 0), a.s.N) : a.s.N;
-    if (q.start < 0) q.n = 0;
-    return q;
-}
-
-// The steps that a row tile visits: [0, sink_steps) and [first, first + steps - sink_steps).
-struct StepRange {
-    int sink_steps, first, steps;
-    DMA_DEV int position(int j) const { return (j < sink_steps ? j : first + j - sink_steps) * STEP; }
-};
-template <int ROWS>
-DMA_DEV StepRange range_of(const CacheAttnArgs& a, const SeqInfo& q, int tile)
-{
-    const int64_t from = (int64_t)q.start + tile * ROWS / a.G, to = (int64_t)q.start + min(q.n - 1, (tile * ROWS + ROWS - 1) / a.G);
-    const int hi = (int)min(to + 1, (int64_t)a.capacity);
-    const int lo = a.window ? (int)min(max(from - a.window + 1, (int64_t)0), (int64_t)hi) : 0;
-    StepRange r;
-    r.first = lo / STEP;
-    r.sink_steps = (min(a.sinks, hi) + STEP - 1) / STEP;
-    if (r.sink_steps >= r.first) r.sink_steps = r.first = 0;
-    r.steps = r.sink_steps + (hi + STEP - 1) / STEP - r.first;
-    return r;
-}
-
-template <bool E5M2, bool HI>
-DMA_DEV int decode2(int w, float sc)
-{
-    if constexpr (E5M2) return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((unsigned)w, sc, HI));
-    else return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w, sc, HI));
-}
-// Eight codes -> eight bf16, an operand of the matrix instruction.
-template <bool E5M2>
-DMA_DEV v8bf decode8(int lo, int hi, float sc)
-{
-    v4i r;
-    r[0] = decode2<E5M2, false>(lo, sc);
-    r[1] = decode2<E5M2, true>(lo, sc);
-    r[2] = decode2<E5M2, false>(hi, sc);
-    r[3] = decode2<E5M2, true>(hi, sc);
-    return __builtin_bit_cast(v8bf, r);
-}
-DMA_DEV float cross_group_max(float x) { return cross_half_max(row_pair_max(x)); }
-DMA_DEV float cross_group_sum(float x)
-{
-    const v2u r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return cross_half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
-DMA_DEV int pack_bf16(float a, float b)
-{
-    v2bf r;
-    r[0] = (__bf16)a;
-    r[1] = (__bf16)b;
-    return __builtin_bit_cast(int, r);
-}
-
-// Bytes that are no number (NaN, infinity): bit 7 of each.
-template <bool E5M2>
-DMA_DEV unsigned no_number(unsigned w) { return ((w & 0x7f7f7f7fu) + (E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u; }
-
-// Bits 0 to 3 -> the four bytes of a dword.
-DMA_DEV int bytes_of(unsigned bits) { return (int)((((bits & 15u) * 0x00204081u) & 0x01010101u) * 0xffu); }
+constexpr int MIN_SHARE = 8;                 // steps: two for each wave
 
 // BY_ITEM: one workgroup per item.  Otherwise the items' steps in equal shares.
 template <int D, bool E5M2, int MT, int W, bool BY_ITEM>
@@ -169,7 +83,11 @@ cache_attn_kernel(CacheAttnArgs a)
             upto = inclusive(mine);
             total += scan[W];
         }
-        const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)a.min_share);
+        // one workgroup per CU instead of two where a share would be short: fewer pieces to join and fewer starts for the same
+        // bytes per CU (one sequence of 32k, 8 kv heads: 23.2 us with 512 shares of 8 steps, 21.7 with 256 of 16; 7 of 0.6k-3k,
+        // 32 heads: 27.9 with 512 of 14, 30.9 with 420 of 16)
+        int64_t share = (total + gridDim.x - 1) / gridDim.x;
+        if (share < 10) share = max((total + gridDim.x / 2 - 1) / (gridDim.x / 2), (int64_t)MIN_SHARE);
         // workgroups next to each other in the line on the same XCD (they are dealt out in turn): they may share a sequence's keys
         const int shares = (int)((total + share - 1) / share), per = (shares + 7) / 8;
         if ((int)(blockIdx.x / 8) >= per) return;
@@ -496,34 +414,45 @@ cache_attn_kernel(CacheAttnArgs a)
     }
 }
 
-// Joins the pieces of split items: a workgroup per item and 4 of its rows; threads over channels (4 each), rows and pieces.
+// Joins the pieces of split items: a workgroup per item and 4 of its rows; threads over channels (4 each), rows and pieces,
+// a thread's loads of several pieces in flight at a time.  Bound by latency: three dependent loads.
 template <int D, int ROWS>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(1024)
 cache_attn_join_kernel(CacheAttnArgs a)
 {
-    constexpr int CH = D / 4, PG = 512 / (4 * CH);
+    constexpr int CH = D / 4, PG = 1024 / (4 * CH), U = 4;
     unsigned item = blockIdx.x;
     const int tile = item % (unsigned)a.row_tiles;
     const int h = item / (unsigned)a.row_tiles % (unsigned)a.c.Hkv, b = item / (unsigned)a.row_tiles / (unsigned)a.c.Hkv;
+    const int2 sp = a.split[item];                              // anything where the item does not exist
     const SeqInfo sq = seq_of(a, b);
-    const int rows = (int)min((int64_t)sq.n * a.G - tile * ROWS, (int64_t)ROWS);
+    const int rows = (int)min((int64_t)sq.n * a.G - (int64_t)tile * ROWS, (int64_t)ROWS);
     const int rr = blockIdx.y * 4 + threadIdx.x / CH % 4, ch = threadIdx.x % CH, pg = threadIdx.x / (4 * CH);
-    if ((int)blockIdx.y * 4 >= rows) return;
-    const int2 sp = a.split[item];
-    if (sp.x == sp.y) return;
+    if ((int)blockIdx.y * 4 >= rows || sp.x == sp.y) return;
     __shared__ v4f os[PG][4][CH];
     __shared__ float ms[PG][4], ls[PG][4];
     v4f o = {0.f, 0.f, 0.f, 0.f};
     float m = M_NONE, l = 0.f;
-    if (rr < rows) {
-        for (int w = sp.x + pg; w <= sp.y; w += PG) {
-            const float* p = a.pieces + (int64_t)(2 * w + (w == sp.x)) * (ROWS * (D + 2));
-            const float m2 = p[ROWS * D + rr], l2 = p[ROWS * D + ROWS + rr], up = fmaxf(m, m2);
-            const v4f x = *(const v4f*)(p + rr * D + ch * 4);
-            const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2 - up) * a.scale);
+    const int r0 = min(rr, rows - 1);
+    for (int w = sp.x + pg; w <= sp.y; w += PG * U) {
+        float m2[U], l2[U];
+        v4f x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int wu = min(w + u * PG, sp.y);
+            const float* p = a.pieces + (int64_t)(2 * wu + (wu == sp.x)) * (ROWS * (D + 2));
+            m2[u] = p[ROWS * D + r0];
+            l2[u] = p[ROWS * D + ROWS + r0];
+            x[u] = *(const v4f*)(p + r0 * D + ch * 4);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (w + u * PG > sp.y) break;
+            const float up = fmaxf(m, m2[u]);
+            const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2[u] - up) * a.scale);
             m = up;
-            l = l * f1 + l2 * f2;
-            o = o * f1 + x * f2;
+            l = l * f1 + l2[u] * f2;
+            o = o * f1 + x[u] * f2;
         }
     }
     os[pg][rr & 3][ch] = o;
@@ -533,7 +462,8 @@ cache_attn_join_kernel(CacheAttnArgs a)
     }
     __syncthreads();
     if (pg || rr >= rows) return;
-    for (int k = 1; k < PG; ++k) {
+    const int groups = min(PG, sp.y - sp.x + 1);
+    for (int k = 1; k < groups; ++k) {
         const float m2 = ms[k][rr & 3], up = fmaxf(m, m2);
         const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2 - up) * a.scale);
         m = up;
@@ -564,8 +494,16 @@ static int cache_cus()
 static int mt_of(int G, int N) { return (int64_t)G * N <= 16 ? 1 : 2; }
 static int64_t grid_of(int mt) { return (int64_t)cache_cus() * 2; }
 
+// Whether the kernel for many rows serves the call.
+static bool many_rows(int B, int Hkv, int G, int N)
+{
+    const int64_t rows = (int64_t)N * G;
+    return rows >= 128 && (int64_t)B * Hkv * ((rows + 127) / 128) >= 128;
+}
+
 size_t cache_attn_workspace(int B, int Hq, int Hkv, int N, int D)
 {
+    if (many_rows(B, Hkv, Hq / Hkv, N)) return 0;
     const int mt = mt_of(Hq / Hkv, N);
     const int64_t tiles = ((int64_t)N * (Hq / Hkv) + 16 * mt - 1) / (16 * mt), items = (int64_t)B * Hkv * tiles;
     return (size_t)(2 * grid_of(mt) * (16 * mt) * (D + 2) * 4 + items * 8);
@@ -576,9 +514,8 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
 {
     constexpr int ROWS = 16 * MT;
     const int64_t tiles = ((int64_t)a.s.N * a.G + ROWS - 1) / ROWS, items = (int64_t)a.s.B * a.c.Hkv * tiles;
-    if (items * 512 > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
+    if (items * (ROWS / 4) * 1024 > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
     a.row_tiles = (int)tiles;
-    a.min_share = 8;
     // the most steps that an item can have
     const int64_t reach = a.window ? std::min((int64_t)a.capacity, (int64_t)a.window + a.sinks + ROWS / a.G + 3 * STEP) : a.capacity;
     if (reach <= 20 * STEP)
@@ -588,7 +525,7 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
     a.split = (int2*)(a.pieces + 2 * grid * ROWS * (D + 2));
     const int rc = launch(cache_attn_kernel<D, E5M2, MT, 4, false>, dim3((unsigned)grid), dim3(256), stream, a);
     if (rc != DMA_OK_) return rc;
-    return launch(cache_attn_join_kernel<D, ROWS>, dim3((unsigned)items, ROWS / 4), dim3(512), stream, a);
+    return launch(cache_attn_join_kernel<D, ROWS>, dim3((unsigned)items, (unsigned)std::min<int64_t>(ROWS / 4, ((int64_t)a.s.N * a.G + 3) / 4)), dim3(1024), stream, a);
 }
 
 int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const Spans& s, int Hq, int window, int sinks,
@@ -604,6 +541,7 @@ int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const 
     a.sinks = window ? sinks : 0;
     a.capacity = c.num_pages ? c.max_pages << c.page_shift : 0;
     a.scale = (float)(1.4426950408889634074 / sqrt((double)c.D));
+    if (many_rows(s.B, c.Hkv, a.G, s.N)) return launch_cache_prompt(a, stream);
     const int mt = mt_of(a.G, s.N);
     auto pick = [&](auto D, auto F) { return mt == 1 ? launch_few<D, F != 0, 1>(a, workspace, stream) : launch_few<D, F != 0, 2>(a, workspace, stream); };
     if (c.D == 128) return c.e5m2 ? pick(IC<128>{}, IC<1>{}) : pick(IC<128>{}, IC<0>{});

@@ -1,0 +1,99 @@
+// What the kernels of the attention over the paged 8-bit cache share.
+#pragma once
+
+#include "dma_device.hpp"
+#include "dma_internal.hpp"
+
+namespace dma {
+
+constexpr int STEP = 64;                     // positions of a step
+constexpr int POS_MAX = 1 << 30;             // above every position that a table holds
+constexpr float M_NONE = -3.0e38f;           // the maximum of nothing: below every score, and finite
+
+struct CacheAttnArgs {
+    CacheView c;
+    Rows q, out;
+    Spans s;
+    int G;                   // query heads per kv head
+    int row_tiles;           // of a sequence with N tokens
+    int window, sinks;
+    int capacity;            // positions that a reader may find
+    float scale;             // log2(e) / sqrt(D)
+    float* pieces;           // few rows: 2 per workgroup: [ROWS][D] sums, then [ROWS] maxima, then [ROWS] weights
+    int2* split;             // ... per item: first and last workgroup that has a piece (first = last: no pieces)
+};
+
+struct SeqInfo {
+    int start, n;
+};
+DMA_DEV SeqInfo seq_of(const CacheAttnArgs& a, int b)
+{
+    SeqInfo q;
+    q.start = a.s.start[b];
+    q.n = a.s.n_tokens ? min(max(a.s.n_tokens[b], 0), a.s.N) : a.s.N;
+    if (q.start < 0) q.n = 0;
+    return q;
+}
+
+// The steps that a row tile visits: [0, sink_steps) and [first, first + steps - sink_steps).
+struct StepRange {
+    int sink_steps, first, steps;
+    DMA_DEV int position(int j) const { return (j < sink_steps ? j : first + j - sink_steps) * STEP; }
+};
+template <int ROWS>
+DMA_DEV StepRange range_of(const CacheAttnArgs& a, const SeqInfo& q, int tile)
+{
+    const int64_t from = (int64_t)q.start + tile * ROWS / a.G, to = (int64_t)q.start + min(q.n - 1, (tile * ROWS + ROWS - 1) / a.G);
+    const int hi = (int)min(to + 1, (int64_t)a.capacity);
+    const int lo = a.window ? (int)min(max(from - a.window + 1, (int64_t)0), (int64_t)hi) : 0;
+    StepRange r;
+    r.first = lo / STEP;
+    r.sink_steps = (min(a.sinks, hi) + STEP - 1) / STEP;
+    if (r.sink_steps >= r.first) r.sink_steps = r.first = 0;
+    r.steps = r.sink_steps + (hi + STEP - 1) / STEP - r.first;
+    return r;
+}
+
+// Two codes (the lower or upper half of a dword) -> two bf16, times the scale: exact.
+template <bool E5M2, bool HI>
+DMA_DEV int decode2(int w, float sc)
+{
+    if constexpr (E5M2) return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((unsigned)w, sc, HI));
+    else return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w, sc, HI));
+}
+// Eight codes -> eight bf16, an operand of the matrix instruction.
+template <bool E5M2>
+DMA_DEV v8bf decode8(int lo, int hi, float sc)
+{
+    v4i r;
+    r[0] = decode2<E5M2, false>(lo, sc);
+    r[1] = decode2<E5M2, true>(lo, sc);
+    r[2] = decode2<E5M2, false>(hi, sc);
+    r[3] = decode2<E5M2, true>(hi, sc);
+    return __builtin_bit_cast(v8bf, r);
+}
+DMA_DEV float cross_group_max(float x) { return cross_half_max(row_pair_max(x)); }
+DMA_DEV float cross_group_sum(float x)
+{
+    const v2u r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return cross_half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+DMA_DEV int pack_bf16(float a, float b)
+{
+    v2bf r;
+    r[0] = (__bf16)a;
+    r[1] = (__bf16)b;
+    return __builtin_bit_cast(int, r);
+}
+
+// Bytes that are no number (NaN, infinity): bit 7 of each.
+template <bool E5M2>
+DMA_DEV unsigned no_number(unsigned w) { return ((w & 0x7f7f7f7fu) + (E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u; }
+
+// Bits 0 to 3 -> the four bytes of a dword.
+DMA_DEV int bytes_of(unsigned bits) { return (int)((((bits & 15u) * 0x00204081u) & 0x01010101u) * 0xffu); }
+
+// Many query rows (dma_cache_prompt.hip).
+int launch_cache_prompt(CacheAttnArgs a, hipStream_t stream);
+
+}  // namespace dma

@@ -223,6 +223,61 @@ def test_windows_of_single_tokens(window, sinks):
     pair.attn(bf16(rng, 5, 8, 1, 128), np.array(lens) - 1, None, window, sinks)
 
 
+@pytest.mark.parametrize("fmt,D,P,G,N", [("e4m3", 128, 64, 2, 100), ("e5m2", 128, 16, 5, 70), ("e4m3", 64, 256, 1, 257), ("e5m2", 64, 32, 4, 33)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 0), (33, 70)])
+def test_many_rows(fmt, D, P, G, N, window, sinks):
+    """Many sequences with pieces of prompts: enough rows for the chip."""
+    rng = np.random.default_rng(N + window)
+    B, Hkv = 18, 4
+    n = rng.integers(0, N + 1, B)
+    n[:3] = N, 1, 0
+    start = rng.integers(0, 200, B)
+    start[:2] = 0
+    start[4] = 700
+    pair = filled(rng, list(start + n), Hkv, P, D, fmt)
+    out = torch.full((B, Hkv * G, N, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    got, rows = pair.attn(bf16(rng, B, Hkv * G, N, D), start, n, window, sinks, out=out)
+    assert (got.float().cpu().numpy()[~rows] == 7).all()
+
+
+@pytest.mark.parametrize("N,G,D,window", [(1, 4, 128, 0), (3, 4, 64, 0), (7, 8, 128, 0), (1, 16, 64, 1500), (9, 2, 128, 2000)])
+def test_long_and_short_sequences_together(N, G, D, window):
+    """More sequences than a workgroup has threads, a few long ones among them: shares that hold many sequences, sequences that
+    take many shares, and some without tokens."""
+    rng = np.random.default_rng(N + G)
+    B = 300
+    start = rng.integers(0, 60, B)
+    start[[0, 7, 150, 299]] = 2900, 1500, 2047, 2500
+    n = np.full(B, N)
+    n[[3, 4, 5, 298]] = 0
+    pair = filled(rng, list(start + n), 1, 64, D, "e4m3")
+    pair.attn(bf16(rng, B, G, N, D), start, n, window, 3)
+    pair.attn(bf16(rng, B, G, N, D), start, np.zeros(B, int), window, 3)       # nothing at all
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("B,Hkv,G,N", [(2, 1, 4, 3), (2, 1, 2, 20), (17, 4, 2, 100)])
+def test_nan_reaches_only_who_sees_it(fmt, B, Hkv, G, N):
+    """A NaN key or value: NaN for the queries behind it, nothing for those before it or whose window has passed it."""
+    rng = np.random.default_rng(40 + N)
+    D, S = 128, 150
+    pair = Pair(rng, [S] * B, Hkv, 64, D, fmt)
+    k, v = bf16(rng, B, Hkv, S, D), bf16(rng, B, Hkv, S, D)
+    v[0, 0, S - N + N // 2, 5] = v[0, 0, S - N + N // 2, 77] = v[1, 0, S - N, 127] = float("nan")
+    k[1, 0, S - 1, 3] = float("nan")
+    pair.write(k, v, [0] * B)
+    pair.same()
+    for window in (0, 2, 70):
+        q = bf16(rng, B, Hkv * G, N, D)
+        got = dma.dma_cache_attn(q.cuda(), pair.gpu, i32([S - N] * B), window=window).double().cpu().numpy()
+        with np.errstate(invalid="ignore"):
+            want, bound = pair.cpu.attn(q.double().numpy(), [S - N] * B, None, window)
+        np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
+        assert np.isnan(want).any() and not np.isnan(want).all()
+        fine = ~np.isnan(want)
+        assert (np.abs(got - want) <= bound)[fine].all()
+
+
 def test_nothing_to_see():
     """Rows whose keys have no page give zeros; sequences without tokens keep their rows."""
     rng = np.random.default_rng(6)
