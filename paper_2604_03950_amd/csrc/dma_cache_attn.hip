@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(64 * W, 2)
 cache_attn_kernel(CacheAttnArgs a)
 {
     constexpr int ROWS = 16 * MT, KJ = D / 64, DT = D / 16, LD = D + 4;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
     __shared__ float obuf[W / 2][ROWS][LD];
     __shared__ float ml[W / 2][2][ROWS];
     __shared__ int64_t scan[W + 1];
@@ -241,36 +241,45 @@ cache_attn_kernel(CacheAttnArgs a)
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[mt][e] = s[mt][e >> 2][e & 3];
-            unsigned seen[MT];                                    // bit e: the lane's 16 positions
-            bool nan_seen = false;                                // some value that a row sees is no number
             if (!plain) {
                 unsigned any = 0;
                 const int base = pos + 16 * grp;
                 auto below = [&](int at) { return (1u << min(max(at - base, 0), 16)) - 1u; };
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
-                    seen[mt] = page_ok ? below(vis_hi[mt] + 1) & (~below(vis_lo[mt]) | below(a.sinks)) : 0u;
-                    any |= seen[mt];
+                    // bit e: the lane's 16 positions
+                    const unsigned seen = page_ok ? below(vis_hi[mt] + 1) & (~below(vis_lo[mt]) | below(a.sinks)) : 0u;
+                    any |= seen;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) x[mt][e] = (seen[mt] >> e) & 1u ? x[mt][e] : -INFINITY;
+                    for (int e = 0; e < 16; ++e) x[mt][e] = (seen >> e) & 1u ? x[mt][e] : -INFINITY;
                 }
                 // over the rows: 16 columns hold different rows of the same positions
                 any |= __builtin_amdgcn_mov_dpp(any, 0x121, 0xF, 0xF, true);
                 any |= __builtin_amdgcn_mov_dpp(any, 0x122, 0xF, 0xF, true);
                 any |= __builtin_amdgcn_mov_dpp(any, 0x124, 0xF, 0xF, true);
                 any |= __builtin_amdgcn_mov_dpp(any, 0x128, 0xF, 0xF, true);
-                // values that no row sees may be anything: zeros instead
-                unsigned bad = 0;
+                // values that no row sees may be anything, and a NaN among the others must not reach the rows that do not see it
+                // through a probability of zero: zeros instead, and NaN in the sums of those who see it
+                bool bad = false;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int keep = bytes_of(any >> (4 * w));
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
                         vr[dt][w] &= keep;
-                        bad |= no_number<E5M2>((unsigned)vr[dt][w]);
+                        const unsigned f = no_number<E5M2>((unsigned)vr[dt][w]);
+                        if (f) bad = true;
+                        vr[dt][w] &= (int)~((f >> 7) * 0xffu);
                     }
                 }
-                nan_seen = __any(bad != 0);
+                if (__any(bad)) {
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        const unsigned long long hit = nan_channels<D, E5M2>(a, b, h, pos, vis_lo[mt], vis_hi[mt], D / 4, [&](int i) { return (i >> 2) * 16 + 4 * grp + (i & 3); });
+#pragma unroll
+                        for (int i = 0; i < D / 4; ++i) o[mt][i >> 2][i & 3] = (hit >> i) & 1 ? NAN : o[mt][i >> 2][i & 3];
+                    }
+                }
             }
             // ---- softmax
             v8bf pf[MT][2];
@@ -299,36 +308,14 @@ cache_attn_kernel(CacheAttnArgs a)
             }
             // ---- values
             const float vsc = __int_as_float(v_scale << 23);
-            if (!nan_seen) {
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
+            for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const v8bf v = decode8<E5M2>(vr[dt][2 * e], vr[dt][2 * e + 1], vsc);
+                for (int e = 0; e < 2; ++e) {
+                    const v8bf v = decode8<E5M2>(vr[dt][2 * e], vr[dt][2 * e + 1], vsc);
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[mt][e], o[mt][dt], 0, 0, 0);
-                    }
-            } else {
-                // It must not reach the rows that do not see it through a probability of zero: row after row, with what the row
-                // does not see taken out.  (A step that all rows see in full has no such rows.)
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll 1
-                    for (int row = 0; row < 16; ++row) {
-                        const unsigned mine = (unsigned)__shfl((int)seen[mt], (lane & 48) + row);
-                        const int keep[4] = {bytes_of(mine), bytes_of(mine >> 4), bytes_of(mine >> 8), bytes_of(mine >> 12)};
-#pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) {
-                            v4f x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                    decode8<E5M2>(vr[dt][2 * e] & keep[2 * e], vr[dt][2 * e + 1] & keep[2 * e + 1], vsc), pf[mt][e], x, 0, 0, 0);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) o[mt][dt][r] += col == row ? x[r] : 0.f;
-                        }
-                    }
-            }
+                    for (int mt = 0; mt < MT; ++mt) o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[mt][e], o[mt][dt], 0, 0, 0);
+                }
             if (j + W < last) load_v(j + W, page_v);
         }
 

@@ -93,6 +93,32 @@ DMA_DEV unsigned no_number(unsigned w) { return ((w & 0x7f7f7f7fu) + (E5M2 ? 0x0
 // Bits 0 to 3 -> the four bytes of a dword.
 DMA_DEV int bytes_of(unsigned bits) { return (int)((((bits & 15u) * 0x00204081u) & 0x01010101u) * 0xffu); }
 
+// Which of a lane's channels have a value that is no number at a position that its row sees, among the 64 from pos: bit i for
+// channel(i).  Read from the cache, a channel after the other: a NaN must reach the rows that see it and, multiplied by a
+// probability of zero, no other, so it is taken out of the matrix product and put into the sums by hand.  Rare, and not fast.
+template <int D, bool E5M2, typename F>
+DMA_DEV unsigned long long nan_channels(const CacheAttnArgs& a, int b, int h, int pos, int vis_lo, int vis_hi, int n, F&& channel)
+{
+    unsigned long long hit = 0;
+#pragma unroll 1
+    for (int g = 0; g < 4; ++g) {
+        const int p = pos + 16 * g, pi = p >> a.c.page_shift;
+        const int page = pi < a.c.max_pages ? a.c.page_table[(int64_t)b * a.c.max_pages + pi] : -1;
+        if (page < 0 || page >= a.c.num_pages) continue;
+        auto below = [&](int at) { return (1u << min(max(at - p, 0), 16)) - 1u; };
+        const unsigned seen = below(vis_hi + 1) & (~below(vis_lo) | below(a.sinks));
+        const uint8_t* base = a.c.v_codes + (((((int64_t)page * a.c.Hkv + h) * D) << a.c.page_shift) + (p & ((1 << a.c.page_shift) - 1)));
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const v4i w = *(const v4i*)(base + (channel(i) << a.c.page_shift));
+            unsigned bad = 0;
+            for (int k = 0; k < 4; ++k) bad |= no_number<E5M2>((unsigned)w[k]) & (unsigned)bytes_of(seen >> (4 * k));
+            if (bad) hit |= 1ull << i;
+        }
+    }
+    return hit;
+}
+
 // Many query rows (dma_cache_prompt.hip).
 int launch_cache_prompt(CacheAttnArgs a, hipStream_t stream);
 

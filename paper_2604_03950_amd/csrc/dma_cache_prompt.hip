@@ -11,7 +11,8 @@
 
 namespace dma {
 
-template <int D, bool E5M2, int NW>
+// UNI: pages of 64 positions and more, so that a step lies in one: its address is the same for all threads.
+template <int D, bool E5M2, int NW, bool UNI>
 __global__ void __launch_bounds__(64 * NW, 2)
 cache_prompt_kernel(CacheAttnArgs a)
 {
@@ -21,7 +22,7 @@ cache_prompt_kernel(CacheAttnArgs a)
     static_assert(KCH >= 1 && VCH >= 1, "");
     __shared__ __attribute__((aligned(16))) char kbuf[2][64 * KROW], vbuf[2][D * VROW];
     __shared__ int odd_in[4];        // of step j at j & 3: bits 0 to 3: 16 positions without a page, bit 4: a value that is no number
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const CacheView& c = a.c;
     const int page_mask = (1 << c.page_shift) - 1;
 
@@ -52,74 +53,100 @@ cache_prompt_kernel(CacheAttnArgs a)
     const int all_hi = cut(wfirst), all_lo = a.window ? cut(wlast - a.window + 1) : 0;
     const int any_hi = cut((int64_t)sq.start + (tile * ROWS + rows - 1) / a.G);
     const int any_lo = a.window ? cut((int64_t)sq.start + tile * ROWS / a.G - a.window + 1) : 0;
+    // ... what all of the workgroup see
+    const int wg_hi = cut((int64_t)sq.start + tile * ROWS / a.G), wg_lo = a.window ? cut((int64_t)sq.start + (tile * ROWS + rows - 1) / a.G - a.window + 1) : 0;
     // ... of the wave: steps without any visible position are skipped
     const int some_lo = a.window ? cut(wfirst - a.window + 1) : 0, some_hi = cut(wlast);
 
     // ---- codes of a step, from memory to registers and from there to LDS
     const int* table = c.page_table + (int64_t)b * c.max_pages;
     v4i kr[KCH], vr[VCH];
-    int kpage[KCH], vpage[VCH], ksc[KCH], vsc[VCH];
-    bool vok[VCH];
+    int kpage[UNI ? 1 : KCH], vpage[UNI ? 1 : VCH], ksc[UNI ? 1 : KCH], vsc[UNI ? 1 : VCH];
+    bool vok[UNI ? 1 : VCH];
+    auto page_at = [&](int p) -> int {
+        const int pi = p >> c.page_shift;
+        return pi < c.max_pages ? table[pi] : -1;
+    };
     auto load_pages = [&](int j) {                                // one step before load(), two before stage()
         const int pos = range.position(j);
-        auto page_at = [&](int p) -> int {
-            const int pi = p >> c.page_shift;
-            return pi < c.max_pages ? table[pi] : -1;
-        };
+        if constexpr (UNI) kpage[0] = page_at(pos);
+        else {
 #pragma unroll
-        for (int u = 0; u < KCH; ++u) kpage[u] = page_at(pos + (threadIdx.x + u * T) / (D / 16));
+            for (int u = 0; u < KCH; ++u) kpage[u] = page_at(pos + (threadIdx.x + u * T) / (D / 16));
 #pragma unroll
-        for (int u = 0; u < VCH; ++u) vpage[u] = page_at(pos + (threadIdx.x & 3) * 16);
+            for (int u = 0; u < VCH; ++u) vpage[u] = page_at(pos + (threadIdx.x & 3) * 16);
+        }
     };
+    const int kofs = threadIdx.x * 16, vofs = (threadIdx.x / 4 << c.page_shift) + (threadIdx.x & 3) * 16;
     auto load = [&](int j) {
         const int pos = range.position(j);
+        if constexpr (UNI) {
+            vok[0] = kpage[0] >= 0 && kpage[0] < c.num_pages;
+            const int64_t slab = (int64_t)(vok[0] ? kpage[0] : 0) * c.Hkv + h;
+            const uint8_t* kb = c.k_codes + ((slab << c.page_shift) + (pos & page_mask)) * D;
+            const uint8_t* vb = c.v_codes + ((slab * D) << c.page_shift) + (pos & page_mask);
 #pragma unroll
-        for (int u = 0; u < KCH; ++u) {
-            const int ch = threadIdx.x + u * T, p = pos + ch / (D / 16);
-            const int64_t slab = (int64_t)(kpage[u] < c.num_pages ? max(kpage[u], 0) : 0) * c.Hkv + h;
-            kr[u] = *(const v4i*)(c.k_codes + (((slab << c.page_shift) + (p & page_mask)) * D + ch % (D / 16) * 16));
-            ksc[u] = c.k_scales[slab];
-        }
+            for (int u = 0; u < KCH; ++u) kr[u] = *(const v4i*)(kb + u * T * 16 + kofs);
 #pragma unroll
-        for (int u = 0; u < VCH; ++u) {
-            const int ch = threadIdx.x + u * T, p = pos + (ch & 3) * 16;
-            vok[u] = vpage[u] >= 0 && vpage[u] < c.num_pages;
-            const int64_t slab = (int64_t)(vok[u] ? vpage[u] : 0) * c.Hkv + h;
-            vr[u] = *(const v4i*)(c.v_codes + (((slab * D + ch / 4) << c.page_shift) + (p & page_mask)));
-            vsc[u] = c.v_scales[slab];
+            for (int u = 0; u < VCH; ++u) vr[u] = *(const v4i*)(vb + ((u * T / 4) << c.page_shift) + vofs);
+            ksc[0] = c.k_scales[slab];
+            vsc[0] = c.v_scales[slab];
+        } else {
+#pragma unroll
+            for (int u = 0; u < KCH; ++u) {
+                const int ch = threadIdx.x + u * T, p = pos + ch / (D / 16);
+                const int64_t slab = (int64_t)(kpage[u] < c.num_pages ? max(kpage[u], 0) : 0) * c.Hkv + h;
+                kr[u] = *(const v4i*)(c.k_codes + (((slab << c.page_shift) + (p & page_mask)) * D + ch % (D / 16) * 16));
+                ksc[u] = c.k_scales[slab];
+            }
+#pragma unroll
+            for (int u = 0; u < VCH; ++u) {
+                const int ch = threadIdx.x + u * T, p = pos + (ch & 3) * 16;
+                vok[u] = vpage[u] >= 0 && vpage[u] < c.num_pages;
+                const int64_t slab = (int64_t)(vok[u] ? vpage[u] : 0) * c.Hkv + h;
+                vr[u] = *(const v4i*)(c.v_codes + (((slab * D + ch / 4) << c.page_shift) + (p & page_mask)));
+                vsc[u] = c.v_scales[slab];
+            }
         }
     };
+    // Rows of LDS are shifted in chunks of 16 bytes so that the 8 lanes of a read's turn find different banks: keys by the number of the
+    // lane that reads them, channels by theirs.
     auto stage = [&](int j, int buf) {
         const int pos = range.position(j);
 #pragma unroll
         for (int u = 0; u < KCH; ++u) {
             const int ch = threadIdx.x + u * T, key = ch / (D / 16), d16 = ch % (D / 16);
-            const float sc = __int_as_float(ksc[u] << 23);
+            const int shift = ((key & 3) | (key >> 1 & 4) | (key << 1 & 8)) & (D / 8 - 1);
+            const float sc = __int_as_float(ksc[UNI ? 0 : u] << 23);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                *(v8bf*)(kbuf[buf] + key * KROW + (((2 * d16 + e) ^ (key & (D / 8 - 1))) * 16)) = decode8<E5M2>(kr[u][2 * e], kr[u][2 * e + 1], sc);
+                *(v8bf*)(kbuf[buf] + key * KROW + ((2 * d16 + e) ^ shift) * 16) = decode8<E5M2>(kr[u][2 * e], kr[u][2 * e + 1], sc);
         }
-        unsigned bad = 0;
+        // Where not all rows see all positions: values that no row sees may be anything, and a NaN among the others must not reach the
+        // rows that do not see it through a probability of zero.  Zeros instead; NaN is put into the sums of those who see it below.
+        const bool open = pos + STEP - 1 <= wg_hi && (pos >= wg_lo || pos + STEP <= a.sinks);
         int odd = 0;
 #pragma unroll
         for (int u = 0; u < VCH; ++u) {
-            const int ch = threadIdx.x + u * T, d = ch / 4, p = pos + (ch & 3) * 16;
-            const float sc = __int_as_float(vsc[u] << 23);
-            if (!vok[u]) odd |= 1 << (ch & 3);
-            // values that no row sees may be anything: zeros instead
-            if (!vok[u] || p + 15 > any_hi || (p < any_lo && p + 16 > a.sinks)) {
-                auto below = [&](int q) { return (1u << min(max(q - p, 0), 16)) - 1u; };
-                const unsigned seen = vok[u] ? below(any_hi + 1) & (~below(any_lo) | below(a.sinks)) : 0u;
+            const int ch = threadIdx.x + u * T, d = ch / 4;
+            const float sc = __int_as_float(vsc[UNI ? 0 : u] << 23);
+            const bool there = vok[UNI ? 0 : u];
+            if (!there) odd |= 1 << (ch & 3);
+            if (!open || !there) {
+                auto below = [&](int q) { return (1u << min(max(q - pos - (ch & 3) * 16, 0), 16)) - 1u; };
+                const unsigned seen = there ? below(any_hi + 1) & (~below(any_lo) | below(a.sinks)) : 0u;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) vr[u][w] &= bytes_of(seen >> (4 * w));
+                for (int w = 0; w < 4; ++w) {
+                    vr[u][w] &= bytes_of(seen >> (4 * w));
+                    const unsigned bad = no_number<E5M2>((unsigned)vr[u][w]);
+                    if (bad) odd |= 16;
+                    vr[u][w] &= (int)~((bad >> 7) * 0xffu);
+                }
             }
 #pragma unroll
-            for (int w = 0; w < 4; ++w) bad |= no_number<E5M2>((unsigned)vr[u][w]);
-#pragma unroll
             for (int e = 0; e < 2; ++e)
-                *(v8bf*)(vbuf[buf] + d * VROW + (((2 * (ch & 3) + e) ^ (d & 7)) * 16)) = decode8<E5M2>(vr[u][2 * e], vr[u][2 * e + 1], sc);
+                *(v8bf*)(vbuf[buf] + d * VROW + ((2 * (ch & 3) + e) ^ (d & 7)) * 16) = decode8<E5M2>(vr[u][2 * e], vr[u][2 * e + 1], sc);
         }
-        if (bad) odd |= 16;
         if (odd) atomicOr(&odd_in[j & 3], odd);
     };
 
@@ -166,7 +193,7 @@ cache_prompt_kernel(CacheAttnArgs a)
                 const char* kp = kbuf[buf] + key * KROW;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
-                    const v8bf k = *(const v8bf*)(kp + (((2 * ks + half) ^ (key & (D / 8 - 1))) * 16));
+                    const v8bf k = *(const v8bf*)(kp + ((2 * ks + half) ^ (col & (D / 8 - 1))) * 16);
                     s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[ks], s[kt], 0, 0, 0);
                 }
             }
@@ -177,85 +204,70 @@ cache_prompt_kernel(CacheAttnArgs a)
                 for (int r = 0; r < 16; ++r) x[kt][r] = s[kt][r];
             // ---- what is not seen
             const bool plain = pos + STEP - 1 <= all_hi && (pos >= all_lo || pos + STEP <= a.sinks) && (odd & 15) == 0;
-            unsigned seen[2] = {0xffffu, 0xffffu};               // bit 8 e + i: position kt * 32 + 16 e + 8 half + i
             if (!plain) {
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
-                    seen[kt] = 0;
+                    unsigned seen = 0;                            // bit 8 e + i: position kt * 32 + 16 e + 8 half + i
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int base = pos + kt * 32 + 16 * e + 8 * half;
                         auto below = [&](int q) { return (1u << min(max(q - base, 0), 8)) - 1u; };
                         const unsigned f = (below(vis_hi + 1) & (~below(vis_lo) | below(a.sinks))) & 0xffu;
-                        seen[kt] |= ((odd >> (2 * kt + e)) & 1 ? 0u : f) << (8 * e);
+                        seen |= ((odd >> (2 * kt + e)) & 1 ? 0u : f) << (8 * e);
                     }
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) x[kt][r] = (seen[kt] >> r) & 1u ? x[kt][r] : -INFINITY;
+                    for (int r = 0; r < 16; ++r) x[kt][r] = (seen >> r) & 1u ? x[kt][r] : -INFINITY;
                 }
             }
-            // ---- softmax
-            float top = x[0][0];
+            // ---- softmax.  The maximum is looked for only where it was too low: the sum of a lane's 32 probabilities shows it
+            // (and is a sum of the rounded ones, as the values' sums are)
+            v8bf pf[4];                                           // positions 16 e + 8 half + [0, 8) of the step
+            float sum;
+            auto probabilities = [&] {
+                const float off = m * a.scale;
+                const v2bf one = __builtin_bit_cast(v2bf, 0x3f803f80);
+                float part[2] = {0.f, 0.f};
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+                for (int e = 0; e < 4; ++e) {
+                    int pw[4];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, x[kt][r]);
-            if (__any((top - m) * a.scale > 8.f)) {
+                    for (int i = 0; i < 4; ++i) {
+                        const float* y = &x[e >> 1][8 * (e & 1) + 2 * i];
+                        pw[i] = pack_bf16(__builtin_amdgcn_exp2f(fmaf(y[0], a.scale, -off)), __builtin_amdgcn_exp2f(fmaf(y[1], a.scale, -off)));
+                        part[i & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, pw[i]), one, part[i & 1], false);
+                    }
+                    pf[e] = __builtin_bit_cast(v8bf, v4i{pw[0], pw[1], pw[2], pw[3]});
+                }
+                sum = part[0] + part[1];
+            };
+            probabilities();
+            if (__any(sum > 1024.f)) {
+                float top = x[0][0];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) top = fmaxf(top, x[kt][r]);
                 const float up = fmaxf(m, cross_half_max(top)), down = __builtin_amdgcn_exp2f((m - up) * a.scale);
                 m = up;
                 l *= down;
 #pragma unroll
                 for (int dt = 0; dt < D / 32; ++dt) o[dt] *= down;
+                probabilities();
             }
-            const float off = m * a.scale;
-            v8bf pf[4];                                           // positions 16 e + 8 half + [0, 8) of the step
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    int pw[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p0 = __builtin_amdgcn_exp2f(fmaf(x[kt][8 * e + 2 * i], a.scale, -off));
-                        const float p1 = __builtin_amdgcn_exp2f(fmaf(x[kt][8 * e + 2 * i + 1], a.scale, -off));
-                        l += p0 + p1;
-                        pw[i] = pack_bf16(p0, p1);
-                    }
-                    pf[2 * kt + e] = __builtin_bit_cast(v8bf, v4i{pw[0], pw[1], pw[2], pw[3]});
-                }
+            l += sum;
             // ---- values
-            if (!(odd & 16) || plain) {
+            if (odd & 16) {
+                const unsigned long long hit = nan_channels<D, E5M2>(a, b, h, pos, vis_lo, vis_hi, D / 2, [&](int i) { return (i >> 4) * 32 + 8 * (i >> 2 & 3) + 4 * half + (i & 3); });
 #pragma unroll
-                for (int dt = 0; dt < D / 32; ++dt) {
-                    const int d = dt * 32 + col;
+                for (int i = 0; i < D / 2; ++i) o[i >> 4][i & 15] = (hit >> i) & 1 ? NAN : o[i >> 4][i & 15];
+            }
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks) {
-                        const v8bf v = *(const v8bf*)(vbuf[buf] + d * VROW + (((2 * ks + half) ^ (d & 7)) * 16));
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[ks], o[dt], 0, 0, 0);
-                    }
-                }
-            } else {
-                // some value is no number: row after row, with what the row does not see taken out
-#pragma unroll 1
-                for (int r = 0; r < 32; ++r) {
-                    const unsigned mine[2] = {(unsigned)__shfl((int)seen[0], (lane & 32) + r), (unsigned)__shfl((int)seen[1], (lane & 32) + r)};
+            for (int dt = 0; dt < D / 32; ++dt) {
+                const int d = dt * 32 + col;
 #pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt) {
-                        const int d = dt * 32 + col;
-                        v16f y;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) y[i] = 0.f;
-#pragma unroll
-                        for (int ks = 0; ks < 4; ++ks) {
-                            const unsigned f = mine[ks >> 1] >> (8 * (ks & 1));
-                            v4i v = *(const v4i*)(vbuf[buf] + d * VROW + (((2 * ks + half) ^ (d & 7)) * 16));
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) v[i] &= (int)(((f >> (2 * i)) & 1u) * 0xffffu | ((f >> (2 * i + 1)) & 1u) * 0xffff0000u);
-                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, v), pf[ks], y, 0, 0, 0);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[dt][i] += col == r ? y[i] : 0.f;
-                        __builtin_amdgcn_sched_barrier(0);        // one channel tile's operands at a time
-                    }
+                for (int ks = 0; ks < 4; ++ks) {
+                    const v8bf v = *(const v8bf*)(vbuf[buf] + d * VROW + ((2 * ks + half) ^ (d & 7)) * 16);
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[ks], o[dt], 0, 0, 0);
                 }
             }
         }
@@ -280,8 +292,12 @@ int launch_cache_prompt(CacheAttnArgs a, hipStream_t stream)
     if (items * 64 * NW > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
     a.row_tiles = (int)tiles;
     const dim3 grid((unsigned)items), block(64 * NW);
-    if (a.c.D == 128) return a.c.e5m2 ? launch(cache_prompt_kernel<128, true, NW>, grid, block, stream, a) : launch(cache_prompt_kernel<128, false, NW>, grid, block, stream, a);
-    return a.c.e5m2 ? launch(cache_prompt_kernel<64, true, NW>, grid, block, stream, a) : launch(cache_prompt_kernel<64, false, NW>, grid, block, stream, a);
+    auto go = [&](auto D, auto E5M2) {
+        return a.c.page_shift >= 6 ? launch(cache_prompt_kernel<D, E5M2 != 0, NW, true>, grid, block, stream, a)
+                                   : launch(cache_prompt_kernel<D, E5M2 != 0, NW, false>, grid, block, stream, a);
+    };
+    if (a.c.D == 128) return a.c.e5m2 ? go(IC<128>{}, IC<1>{}) : go(IC<128>{}, IC<0>{});
+    return a.c.e5m2 ? go(IC<64>{}, IC<1>{}) : go(IC<64>{}, IC<0>{});
 }
 
 }  // namespace dma
