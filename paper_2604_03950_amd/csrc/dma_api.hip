@@ -42,6 +42,7 @@ int check_cache(const dma_kv_cache* cache, int B, int N, dma::CacheView& c)
     c.k_scales = (uint8_t*)cache->k_scales; c.v_scales = (uint8_t*)cache->v_scales;
     c.page_table = (const int*)cache->page_table;
     c.num_pages = cache->num_pages;
+    c.page_limit = (unsigned)(cache->num_pages < 0x7fffffff ? cache->num_pages : 0x80000000LL);
     c.max_pages = cache->max_pages;
     c.page_shift = __builtin_ctz((unsigned)P);
     c.Hkv = cache->Hkv;

@@ -40,7 +40,7 @@ DMA_DEV bool find_item(const CacheView& c, const Spans& s, int pages_per_seq, Pa
     it.first = pi << c.page_shift;
     if (it.first >= end) return false;            // (pi < max_pages follows from it)
     const int page = c.page_table[(int64_t)it.b * c.max_pages + pi];
-    if (page < 0 || page >= c.num_pages) return false;
+    if ((unsigned)page >= c.page_limit) return false;
     it.lo = max(it.start - it.first, 0);
     it.hi = min(end - it.first, P);
     it.slab = (int64_t)page * c.Hkv + it.h;

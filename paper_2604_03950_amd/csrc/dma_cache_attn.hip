@@ -171,7 +171,7 @@ cache_attn_kernel(CacheAttnArgs a)
             const int pi = (range.position(j) + 16 * g) >> c.page_shift;
             return pi < c.max_pages ? table[pi] : -1;
         };
-        auto slab_of = [&](int page) -> int64_t { return (int64_t)((page >= 0 && page < c.num_pages) ? page : 0) * c.Hkv + h; };
+        auto slab_of = [&](int page) -> int64_t { return (int64_t)((unsigned)page < c.page_limit ? page : 0) * c.Hkv + h; };
         v4i kr[4][KJ], vr[DT];
         int k_scale, v_scale, v_page;
         auto load_k = [&](int j, int page) {
@@ -207,7 +207,7 @@ cache_attn_kernel(CacheAttnArgs a)
         }
         for (; j < last; j += W) {
             const int pos = range.position(j);
-            const bool page_ok = v_page >= 0 && v_page < c.num_pages;
+            const bool page_ok = (unsigned)v_page < c.page_limit;
             // ---- scores
             v4f s[MT][4];
 #pragma unroll

@@ -104,7 +104,7 @@ DMA_DEV unsigned long long nan_channels(const CacheAttnArgs& a, int b, int h, in
     for (int g = 0; g < 4; ++g) {
         const int p = pos + 16 * g, pi = p >> a.c.page_shift;
         const int page = pi < a.c.max_pages ? a.c.page_table[(int64_t)b * a.c.max_pages + pi] : -1;
-        if (page < 0 || page >= a.c.num_pages) continue;
+        if ((unsigned)page >= a.c.page_limit) continue;
         auto below = [&](int at) { return (1u << min(max(at - p, 0), 16)) - 1u; };
         const unsigned seen = below(vis_hi + 1) & (~below(vis_lo) | below(a.sinks));
         const uint8_t* base = a.c.v_codes + (((((int64_t)page * a.c.Hkv + h) * D) << a.c.page_shift) + (p & ((1 << a.c.page_shift) - 1)));

@@ -81,7 +81,7 @@ cache_prompt_kernel(CacheAttnArgs a)
     auto load = [&](int j) {
         const int pos = range.position(j);
         if constexpr (UNI) {
-            vok[0] = kpage[0] >= 0 && kpage[0] < c.num_pages;
+            vok[0] = (unsigned)kpage[0] < c.page_limit;
             const int64_t slab = (int64_t)(vok[0] ? kpage[0] : 0) * c.Hkv + h;
             const uint8_t* kb = c.k_codes + ((slab << c.page_shift) + (pos & page_mask)) * D;
             const uint8_t* vb = c.v_codes + ((slab * D) << c.page_shift) + (pos & page_mask);
@@ -95,28 +95,29 @@ cache_prompt_kernel(CacheAttnArgs a)
 #pragma unroll
             for (int u = 0; u < KCH; ++u) {
                 const int ch = threadIdx.x + u * T, p = pos + ch / (D / 16);
-                const int64_t slab = (int64_t)(kpage[u] < c.num_pages ? max(kpage[u], 0) : 0) * c.Hkv + h;
+                const int64_t slab = (int64_t)((unsigned)kpage[u] < c.page_limit ? kpage[u] : 0) * c.Hkv + h;
                 kr[u] = *(const v4i*)(c.k_codes + (((slab << c.page_shift) + (p & page_mask)) * D + ch % (D / 16) * 16));
                 ksc[u] = c.k_scales[slab];
             }
 #pragma unroll
             for (int u = 0; u < VCH; ++u) {
                 const int ch = threadIdx.x + u * T, p = pos + (ch & 3) * 16;
-                vok[u] = vpage[u] >= 0 && vpage[u] < c.num_pages;
+                vok[u] = (unsigned)vpage[u] < c.page_limit;
                 const int64_t slab = (int64_t)(vok[u] ? vpage[u] : 0) * c.Hkv + h;
                 vr[u] = *(const v4i*)(c.v_codes + (((slab * D + ch / 4) << c.page_shift) + (p & page_mask)));
                 vsc[u] = c.v_scales[slab];
             }
         }
     };
-    // Rows of LDS are shifted in chunks of 16 bytes so that the 8 lanes of a read's turn find different banks: keys by the number of the
-    // lane that reads them, channels by theirs.
+    // Rows of LDS are shifted in chunks of 16 bytes so that the 16 lanes of a read's turn find different banks (256 bytes of them: one
+    // row, or two of 128 bytes): keys by the number of the lane that reads them, channels by theirs.
+    auto shift_of = [](int lane_row, int row_bytes) { return row_bytes == 256 ? lane_row & 15 : lane_row >> 1 & 7; };
     auto stage = [&](int j, int buf) {
         const int pos = range.position(j);
 #pragma unroll
         for (int u = 0; u < KCH; ++u) {
             const int ch = threadIdx.x + u * T, key = ch / (D / 16), d16 = ch % (D / 16);
-            const int shift = ((key & 3) | (key >> 1 & 4) | (key << 1 & 8)) & (D / 8 - 1);
+            const int shift = shift_of((key & 3) | (key >> 1 & 4) | (key << 1 & 8), KROW);
             const float sc = __int_as_float(ksc[UNI ? 0 : u] << 23);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
@@ -145,7 +146,7 @@ cache_prompt_kernel(CacheAttnArgs a)
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                *(v8bf*)(vbuf[buf] + d * VROW + ((2 * (ch & 3) + e) ^ (d & 7)) * 16) = decode8<E5M2>(vr[u][2 * e], vr[u][2 * e + 1], sc);
+                *(v8bf*)(vbuf[buf] + d * VROW + ((2 * (ch & 3) + e) ^ shift_of(d, VROW)) * 16) = decode8<E5M2>(vr[u][2 * e], vr[u][2 * e + 1], sc);
         }
         if (odd) atomicOr(&odd_in[j & 3], odd);
     };
@@ -172,6 +173,13 @@ cache_prompt_kernel(CacheAttnArgs a)
     __syncthreads();
     // S rows of lane half `half`: register 4 q + i is row 8 q + 4 half + i of the 32, and holds position 16 (q / 2) + 8 half + 4 (q & 1) + i
     const int key_of_row = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+    // the queries have arrived before the loop: no wait for them inside it, which would be one for the codes requested meanwhile
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        v4i w = __builtin_bit_cast(v4i, qf[ks]);
+        asm volatile("" : "+v"(w));
+        qf[ks] = __builtin_bit_cast(v8bf, w);
+    }
     for (int j = 0; j < range.steps; ++j) {
         const int buf = j & 1, pos = range.position(j);
         if (j + 1 < range.steps) {
@@ -185,18 +193,28 @@ cache_prompt_kernel(CacheAttnArgs a)
         if (!none) {
             // ---- scores
             v16f s[2];
+            v8bf kf[2][D / 16];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const char* kp = kbuf[buf] + (kt * 32 + key_of_row) * KROW;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) kf[kt][ks] = *(const v8bf*)(kp + ((2 * ks + half) ^ shift_of(col, KROW)) * 16);
+            }
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
-                const int key = kt * 32 + key_of_row;
-                const char* kp = kbuf[buf] + key * KROW;
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const v8bf k = *(const v8bf*)(kp + ((2 * ks + half) ^ (col & (D / 8 - 1))) * 16);
-                    s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[ks], s[kt], 0, 0, 0);
-                }
+                for (int ks = 0; ks < D / 16; ++ks) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kt][ks], qf[ks], s[kt], 0, 0, 0);
             }
+            // half of the operands ahead, the rest between the products
+            __builtin_amdgcn_sched_group_barrier(0x100, D / 16, 0);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, D / 16, 0);
             float x[2][16];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
@@ -261,15 +279,22 @@ cache_prompt_kernel(CacheAttnArgs a)
 #pragma unroll
                 for (int i = 0; i < D / 2; ++i) o[i >> 4][i & 15] = (hit >> i) & 1 ? NAN : o[i >> 4][i & 15];
             }
+            v8bf vf[D / 32][4];
 #pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt) {
-                const int d = dt * 32 + col;
+            for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks) {
-                    const v8bf v = *(const v8bf*)(vbuf[buf] + d * VROW + ((2 * ks + half) ^ (d & 7)) * 16);
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[ks], o[dt], 0, 0, 0);
-                }
+                for (int ks = 0; ks < 4; ++ks) vf[dt][ks] = *(const v8bf*)(vbuf[buf] + (dt * 32 + col) * VROW + ((2 * ks + half) ^ shift_of(col, VROW)) * 16);
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt][ks], pf[ks], o[dt], 0, 0, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 1);
+#pragma unroll
+            for (int i = 0; i < D / 8 - 6; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
             }
+            __builtin_amdgcn_sched_group_barrier(0x008, 6, 1);
         }
         __syncthreads();
     }

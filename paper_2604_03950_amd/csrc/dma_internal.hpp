@@ -60,6 +60,7 @@ struct CacheView {
     uint8_t* v_scales;
     const int* page_table;
     int64_t num_pages;
+    unsigned page_limit;     // a page number below it, as unsigned, is one of the cache's
     int max_pages, page_shift, Hkv, D;
     bool e5m2;
 };
