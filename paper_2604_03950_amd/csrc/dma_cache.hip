@@ -2,8 +2,8 @@
 //
 // A workgroup takes the keys or the values of one page of one kv head, and holds all of it in registers: a thread has four
 // chunks of 8 elements (16 bytes).  For keys, consecutive threads have consecutive chunks; for values a thread's four chunks
-// are the same 8 channels of four consecutive positions, so that the codes of a channel leave as whole dwords (positions lie
-// innermost), 16 threads covering 64 consecutive bytes and 4 of them 64 bytes of a row on the other side.
+// are the same 8 channels of four consecutive positions, so that the codes of a channel are whole dwords (positions lie
+// innermost).  A whole page's values go through LDS, where they are turned, and cross memory in one piece.
 #include "dma_cache_device.hpp"
 #include <algorithm>
 
@@ -47,25 +47,36 @@ DMA_DEV bool find_item(const CacheView& c, const Spans& s, int pages_per_seq, Pa
     return true;
 }
 
+// Dword of the value codes of (channel d, positions 4 quad ..) in LDS: rows of 1 << page_shift bytes.  The rows of a group of 8 channels
+// are permuted by the group's number, and the 16-byte chunks of a row by that of 32 channels, so that the threads of a wave (all channel
+// groups of 16 or 32 positions) write to different banks.
+DMA_DEV int turned(int page_shift, int d, int quad)
+{
+    return ((d ^ ((d >> 3) & 7)) << (page_shift - 2)) + (quad ^ ((d >> 5) << 2 & ((1 << (page_shift - 2)) - 4)));
+}
+
 // Place and channel group of chunk u of this thread.
 template <int D>
 DMA_DEV void chunk_of(int kv, int page_shift, int u, int& place, int& dch)
 {
-    const int P = 1 << page_shift;
     if (kv == 0) {
-        const int ch = threadIdx.x + u * ((P / 4) * (D / 8));
+        const int ch = threadIdx.x + u * ((1 << page_shift) / 4 * (D / 8));
         place = ch / (D / 8);
         dch = ch % (D / 8);
     } else {
-        const int quads = min(P / 4, 16), r = threadIdx.x / quads;
-        dch = r % (D / 8);
-        place = 4 * ((r / (D / 8)) * quads + threadIdx.x % quads) + u;
+        place = 4 * (threadIdx.x / (D / 8)) + u;
+        dch = threadIdx.x % (D / 8);
     }
 }
 
+// Eight bf16 -> eight codes, divided by the power of two in sc, to nearest even.  (By way of binary32: the convert that reads packed bf16
+// saves 32 of some 190 vector instructions of a thread and costs time, 64 rows of 128 at a time 42.4 us against 40.0 for 201 MB: the
+// kernel is bound by memory.)
 template <bool E5M2>
-DMA_DEV v2i encode8_cache(const float (&x)[8], float sc)
+DMA_DEV v2i encode8_cache(const v4i& w, float sc)
 {
+    float x[8];
+    unpack8<false>(w, 1.f, x);
     v2s a = {0, 0}, b = {0, 0};
     if constexpr (E5M2) {
         a = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(a, x[0], x[1], sc, false);
@@ -78,10 +89,18 @@ DMA_DEV v2i encode8_cache(const float (&x)[8], float sc)
         b = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(b, x[4], x[5], sc, false);
         b = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(b, x[6], x[7], sc, true);
     }
-    v2i r;
-    r[0] = __builtin_bit_cast(int, a);
-    r[1] = __builtin_bit_cast(int, b);
-    return r;
+    return v2i{__builtin_bit_cast(int, a), __builtin_bit_cast(int, b)};
+}
+
+// Four dwords of four bytes, turned: byte u of r[i] is byte i of w[u].
+DMA_DEV void turn4(const unsigned (&w)[4], unsigned (&r)[4])
+{
+    const unsigned a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+    const unsigned c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    r[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    r[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    r[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    r[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
 // Four codes rounded once more, to element * 2^-by (by > 0: nothing can overflow).  down: 2^-by.
@@ -142,28 +161,21 @@ kv_write_kernel(CacheView c, Rows k, Rows v, Spans s, int pages_per_seq)
     const int P = 1 << c.page_shift;
     const bool active = threadIdx.x < (P / 4) * (D / 8);        // all but for pages of 16 at D = 64: half a wave
     v4i w[4];
-    unsigned top = 0;                                           // largest finite magnitude
-    bool odd = false;                                           // something above 1.75 * 2^127
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         int place, dch;
         chunk_of<D>(it.kv, c.page_shift, u, place, dch);
         w[u] = v4i{0, 0, 0, 0};
         if (active && place >= it.lo && place < it.hi)
-            w[u] = *(const v4i*)(row0 + (int64_t)(it.first + place - it.start) * src.stride_token + dch * 16);
+            w[u] = __builtin_nontemporal_load((const v4i*)(row0 + (int64_t)(it.first + place - it.start) * src.stride_token + dch * 16));
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const unsigned a = amax8_bf16_packed(w[u]);
-        unsigned m = max(a & 0xffffu, a >> 16);
-        odd |= m > 0x7f60u;
-        if (m >= 0x7f80u) m = amax8_finite(w[u]);
-        top = max(top, m);
-    }
+    const unsigned two = pk_max_u16(pk_max_u16(amax8_bf16_packed(w[0]), amax8_bf16_packed(w[1])), pk_max_u16(amax8_bf16_packed(w[2]), amax8_bf16_packed(w[3])));
+    unsigned top = max(two & 0xffffu, two >> 16);               // largest finite magnitude, a bf16 pattern
+    const bool odd = top > 0x7f60u;                             // something above 1.75 * 2^127
+    if (top >= 0x7f80u) top = max(max(amax8_finite(w[0]), amax8_finite(w[1])), max(amax8_finite(w[2]), amax8_finite(w[3])));
     // largest of the workgroup
     __shared__ unsigned wave_top[16];
-#pragma unroll
-    for (int x = 32; x; x >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, x));
+    top = __float_as_uint(cross_half_max(row_pair_max(group_max<16>(__uint_as_float(top << 16))))) >> 16;
     if ((threadIdx.x & 63) == 0) wave_top[threadIdx.x >> 6] = top;
     const int before = it.lo ? *scale_at : 0;                   // every thread reads it before one replaces it
     __syncthreads();
@@ -180,17 +192,18 @@ kv_write_kernel(CacheView c, Rows k, Rows v, Spans s, int pages_per_seq)
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         if (odd) w[u] = clamp8(w[u], min((unsigned)((scale + EMAX) << 7) | 96u, 0x7f60u));
-        float x[8];
-        unpack8<false>(w[u], 1.f, x);
-        q[u] = encode8_cache<E5M2>(x, sc);
+        q[u] = encode8_cache<E5M2>(w[u], sc);
     }
+    // whole pages pass the caches by: a prompt is larger than they are (201 MB with its codes kept in them 36.1 us, without 34.2)
+    const bool full = it.lo == 0 && it.hi == P;                 // the same for the whole workgroup
     if (it.kv == 0) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             int place, dch;
             chunk_of<D>(0, c.page_shift, u, place, dch);
             v2i* at = (v2i*)(codes + place * D + dch * 8);
-            if (place >= it.lo && place < it.hi) *at = q[u];
+            if (full) __builtin_nontemporal_store(q[u], at);
+            else if (place >= it.lo && place < it.hi) *at = q[u];
             else if (grown && place < it.lo) {
                 v2i old = *at;
                 old[0] = (int)recode4<E5M2>((unsigned)old[0], down);
@@ -202,6 +215,24 @@ kv_write_kernel(CacheView c, Rows k, Rows v, Spans s, int pages_per_seq)
         int place, dch;
         chunk_of<D>(1, c.page_shift, 0, place, dch);
         uint8_t* col = codes + ((dch * 8) << c.page_shift) + place;
+        unsigned w4[8];                                         // of channel i, the four positions
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const unsigned in[4] = {(unsigned)q[0][i >> 2], (unsigned)q[1][i >> 2], (unsigned)q[2][i >> 2], (unsigned)q[3][i >> 2]};
+            unsigned r[4];
+            turn4(in, r);
+            w4[i] = r[0]; w4[i + 1] = r[1]; w4[i + 2] = r[2]; w4[i + 3] = r[3];
+        }
+        if (full) {
+            extern __shared__ __attribute__((aligned(16))) unsigned tile[];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) tile[turned(c.page_shift, dch * 8 + i, place / 4)] = w4[i];
+            __syncthreads();
+            const int n16 = (P * D) >> 4;
+            for (int ch = threadIdx.x; ch < n16; ch += (P / 4) * (D / 8))
+                __builtin_nontemporal_store(*(const v4i*)&tile[turned(c.page_shift, ch >> (c.page_shift - 4), (ch & (P / 16 - 1)) * 4)], (v4i*)codes + ch);
+            return;
+        }
         const bool all = place >= it.lo && place + 4 <= it.hi;
         if (!all && grown && place < it.lo) {                   // earlier tokens of this quad first
 #pragma unroll
@@ -213,16 +244,12 @@ kv_write_kernel(CacheView c, Rows k, Rows v, Spans s, int pages_per_seq)
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int sh = 8 * (i & 3);
             uint8_t* at = col + (i << c.page_shift);
-            unsigned byte[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) byte[u] = ((unsigned)q[u][i >> 2] >> sh) & 0xffu;
-            if (all) *(unsigned*)at = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
+            if (all) *(unsigned*)at = w4[i];
             else {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
-                    if (place + u >= it.lo && place + u < it.hi) at[u] = (uint8_t)byte[u];
+                    if (place + u >= it.lo && place + u < it.hi) at[u] = (uint8_t)(w4[i] >> (8 * u));
             }
         }
     }
@@ -257,10 +284,14 @@ kv_read_kernel(CacheView c, Rows k, Rows v, Spans s, int pages_per_seq)
     } else {
         int place, dch;
         chunk_of<D>(1, c.page_shift, 0, place, dch);
-        const uint8_t* col = codes + ((dch * 8) << c.page_shift) + place;
+        extern __shared__ __attribute__((aligned(16))) unsigned tile[];
+        const int n16 = (P * D) >> 4;
+        for (int ch = threadIdx.x; ch < n16; ch += (P / 4) * (D / 8))
+            *(v4i*)&tile[turned(c.page_shift, ch >> (c.page_shift - 4), (ch & (P / 16 - 1)) * 4)] = ((const v4i*)codes)[ch];
+        __syncthreads();
         unsigned w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = *(const unsigned*)(col + (i << c.page_shift));
+        for (int i = 0; i < 8; ++i) w[i] = tile[turned(c.page_shift, dch * 8 + i, place / 4)];
         // the bytes of two channels side by side: positions 0 and 1, then 2 and 3
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
@@ -276,7 +307,7 @@ kv_read_kernel(CacheView c, Rows k, Rows v, Spans s, int pages_per_seq)
         int place, dch;
         chunk_of<D>(it.kv, c.page_shift, u, place, dch);
         if (place >= it.lo && place < it.hi)
-            *(v4i*)(row0 + (int64_t)(it.first + place - it.start) * dst.stride_token + dch * 16) = out[u];
+            __builtin_nontemporal_store(out[u], (v4i*)(row0 + (int64_t)(it.first + place - it.start) * dst.stride_token + dch * 16));
     }
 }
 
@@ -292,7 +323,7 @@ static int launch_pages(K* const (&kernels)[2][2], const CacheView& c, const Row
     if (pages > (int64_t)0x7fffffff / per_page || s.B > (int64_t)0x7fffffff / (per_page * pages)) return DMA_ERR_UNSUPPORTED_;
     const int64_t blocks = per_page * pages * s.B;
     if (blocks * threads > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;       // what a launch may hold
-    return launch(kernels[c.D == 128][c.e5m2], dim3((unsigned)blocks), dim3(threads), stream, c, k, v, s, (int)pages);
+    return launch_lds(kernels[c.D == 128][c.e5m2], dim3((unsigned)blocks), dim3(threads), P * c.D, stream, c, k, v, s, (int)pages);
 }
 
 int launch_kv_write(const CacheView& c, const Rows& k, const Rows& v, const Spans& s, hipStream_t stream)

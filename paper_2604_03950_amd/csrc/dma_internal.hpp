@@ -19,18 +19,24 @@ constexpr int DMA_ERR_HIP_ = -3;
 // Launch `kernel` and report what THIS launch returned: DMA_OK_ or DMA_ERR_HIP_.  (hipGetLastError() after a <<<>>> launch
 // would also report, and clear, an error some earlier, unrelated HIP call of the caller's thread left behind.)
 template <typename... P, size_t... I>
-inline hipError_t launch_impl(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t stream, std::tuple<P...>& vals,
+inline hipError_t launch_impl(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t stream, std::tuple<P...>& vals,
                               std::index_sequence<I...>)
 {
     void* ptrs[] = {static_cast<void*>(&std::get<I>(vals))...};
-    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, ptrs, 0, stream);
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, ptrs, lds, stream);
+}
+// ... with `lds` bytes of shared memory beyond what the kernel declares.
+template <typename... P, typename... A>
+inline int launch_lds(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t stream, A... args)
+{
+    static_assert(sizeof...(P) == sizeof...(A), "one argument per kernel parameter");
+    std::tuple<P...> vals{static_cast<P>(args)...};
+    return launch_impl(kernel, grid, block, lds, stream, vals, std::index_sequence_for<P...>{}) == hipSuccess ? DMA_OK_ : DMA_ERR_HIP_;
 }
 template <typename... P, typename... A>
 inline int launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t stream, A... args)
 {
-    static_assert(sizeof...(P) == sizeof...(A), "one argument per kernel parameter");
-    std::tuple<P...> vals{static_cast<P>(args)...};
-    return launch_impl(kernel, grid, block, stream, vals, std::index_sequence_for<P...>{}) == hipSuccess ? DMA_OK_ : DMA_ERR_HIP_;
+    return launch_lds(kernel, grid, block, 0, stream, args...);
 }
 
 // mode: 1 = E4M3 only (c8/s8), 2 = E2M1 only (c4/s4), 3 = both, 4 = E5M2 only (c8/s8).
