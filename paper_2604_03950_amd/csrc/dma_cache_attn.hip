@@ -7,8 +7,8 @@
 // innermost).  Codes go from memory to registers once and are decoded to bf16 there, times the page's scale (exact); no LDS until
 // the waves of a workgroup, which take turns at the steps, join their sums.
 //
-// Softmax: base 2, one maximum per row, raised only when a score exceeds it by 8 units (then everything is scaled down): p <= 2^8,
-// which neither binary32 sums nor bf16's rounding of p notice, and a step needs no exchange between lanes.
+// Softmax: base 2, one maximum per row, raised only where it was far too low (then everything is scaled down): p <= 2^10, which
+// neither binary32 sums nor bf16's rounding of p notice, and a step needs no exchange between lanes.
 //
 // Long and uneven sequences: the steps of all (sequence, kv head, row tile) items form one line that is cut into equal shares, one
 // per workgroup.  An item that lies in one share is written directly; pieces of the others go to the workspace, and a second
@@ -23,7 +23,8 @@ namespace dma {
 constexpr int MIN_SHARE = 8;                 // steps: two for each wave
 
 // BY_ITEM: one workgroup per item.  Otherwise the items' steps in equal shares.
-template <int D, bool E5M2, int MT, int W, bool BY_ITEM>
+// UNI: pages of 64 positions and more, so that a step lies in one: its page is the same for all lanes.
+template <int D, bool E5M2, int MT, int W, bool BY_ITEM, bool UNI>
 __global__ void __launch_bounds__(64 * W, 2)
 cache_attn_kernel(CacheAttnArgs a)
 {
@@ -165,31 +166,41 @@ cache_attn_kernel(CacheAttnArgs a)
             l[mt] = 0.f;
         }
 
+        __builtin_amdgcn_sched_barrier(0);
         // Pages of a step: of the 16 positions whose keys this lane loads, and of those whose values it loads.
         const int* table = c.page_table + (int64_t)b * c.max_pages;
         auto page_of = [&](int j, int g) -> int {
-            const int pi = (range.position(j) + 16 * g) >> c.page_shift;
-            return pi < c.max_pages ? table[pi] : -1;
+            const int pi = (range.position(j) + (UNI ? 0 : 16 * g)) >> c.page_shift;
+            const int at = min(pi, c.max_pages - 1);
+            const int page = UNI ? scalar_at(table, __builtin_amdgcn_readfirstlane(at)) : table[at];
+            return pi < c.max_pages ? page : -1;
         };
-        auto slab_of = [&](int page) -> int64_t { return (int64_t)((unsigned)page < c.page_limit ? page : 0) * c.Hkv + h; };
+        auto slab_of = [&](int page) -> int64_t {
+            if constexpr (UNI) page = __builtin_amdgcn_readfirstlane(page);
+            return (int64_t)((unsigned)page < c.page_limit ? page : 0) * c.Hkv + h;
+        };
         v4i kr[4][KJ], vr[DT];
-        int k_scale, v_scale, v_page;
-        auto load_k = [&](int j, int page) {
+        uint8_t k_scale, v_scale;
+        int v_page;
+        // the positions of a lane's keys: 16 (col / 4) + 4 t + col % 4 in product t
+        auto load_k = [&](int j, int page, bool on) {
             const int64_t slab = slab_of(page);
-            const int place = ((range.position(j) + 16 * (col >> 2)) & page_mask) + (col & 3);
-            const uint8_t* p = c.k_codes + (((slab << c.page_shift) + place) * D + grp * 16);
+            const int pos = range.position(j), at = 16 * (col >> 2);
+            const uint8_t* base = c.k_codes + ((slab << c.page_shift) + ((UNI ? pos : pos + at) & page_mask)) * D;
+            const uint8_t* p = base + (on ? (unsigned)(((UNI ? at : 0) + (col & 3)) * D + grp * 16) : 0u);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int jj = 0; jj < KJ; ++jj) kr[t][jj] = *(const v4i*)(p + t * 4 * D + jj * 64);
             k_scale = c.k_scales[slab];
         };
-        auto load_v = [&](int j, int page) {
+        auto load_v = [&](int j, int page, bool on) {
             const int64_t slab = slab_of(page);
-            const int place = (range.position(j) + 16 * grp) & page_mask;
-            const uint8_t* p = c.v_codes + (((slab * D + col) << c.page_shift) + place);
+            const int pos = range.position(j);
+            const uint8_t* base = c.v_codes + ((slab * D) << c.page_shift) + ((UNI ? pos : pos + 16 * grp) & page_mask);
+            const unsigned mine = on ? (col << c.page_shift) + (UNI ? 16 * grp : 0) : 0u;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) vr[dt] = *(const v4i*)(p + ((dt * 16) << c.page_shift));
+            for (int dt = 0; dt < DT; ++dt) vr[dt] = *(const v4i*)(base + ((dt * 16) << c.page_shift) + mine);
             v_scale = c.v_scales[slab];
             v_page = page;
         };
@@ -198,14 +209,27 @@ cache_attn_kernel(CacheAttnArgs a)
         int j = skip + wave;
         int pk = -1, pv = -1;                                     // pages of the step after the next
         if (j < last) {
-            load_k(j, page_of(j, col >> 2));
-            load_v(j, page_of(j, grp));
-            if (j + W < last) {
-                pk = page_of(j + W, col >> 2);
-                pv = page_of(j + W, grp);
-            }
+            pk = page_of(j, col >> 2);
+            pv = UNI ? pk : page_of(j, grp);
+            load_k(j, pk, true);
+            load_v(j, pv, true);
+            pk = page_of(min(j + W, last - 1), col >> 2);
+            pv = UNI ? pk : page_of(min(j + W, last - 1), grp);
         }
+        // the queries, requested first, have arrived before the loop: no wait for them inside it, which would be one for the codes
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int ks = 0; ks < 2 * KJ; ++ks) {
+                v4i w = __builtin_bit_cast(v4i, qf[mt][ks]);
+                asm volatile("" : "+v"(w));
+                qf[mt][ks] = __builtin_bit_cast(v8bf, w);
+            }
         for (; j < last; j += W) {
+            // the codes of the next step are requested without a branch (what the compiler cannot count it waits for in full):
+            // behind the last step, one address for all lanes
+            const int next = min(j + W, last - 1);
+            const bool more = j + W < last;
             const int pos = range.position(j);
             const bool page_ok = (unsigned)v_page < c.page_limit;
             // ---- scores
@@ -227,13 +251,9 @@ cache_attn_kernel(CacheAttnArgs a)
                     }
             // ---- the next step's keys, the pages of the one after it
             const int page_v = pv;
-            if (j + W < last) {
-                load_k(j + W, pk);
-                if (j + 2 * W < last) {
-                    pk = page_of(j + 2 * W, col >> 2);
-                    pv = page_of(j + 2 * W, grp);
-                }
-            }
+            load_k(next, pk, more);
+            pk = page_of(min(j + 2 * W, last - 1), col >> 2);
+            pv = UNI ? pk : page_of(min(j + 2 * W, last - 1), grp);
             // ---- what is not seen
             const bool plain = pos + STEP - 1 <= all_hi && (pos >= all_lo || pos + STEP <= a.sinks) && __all(page_ok);
             float x[MT][16];                                      // position 16 grp + 4 t + r of the step at 4 t + r
@@ -285,24 +305,34 @@ cache_attn_kernel(CacheAttnArgs a)
             v8bf pf[MT][2];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                float top = x[mt][0];
+                // the maximum is looked for only where it was too low: the sum of a lane's 16 probabilities shows it (and is a sum of
+                // the rounded ones, as the values' sums are)
+                int pw[8];
+                float sum;
+                auto probabilities = [&] {
+                    const float off = m[mt] * a.scale;
+                    const v2bf one = __builtin_bit_cast(v2bf, 0x3f803f80);
+                    float part[2] = {0.f, 0.f};
 #pragma unroll
-                for (int e = 1; e < 16; ++e) top = fmaxf(top, x[mt][e]);
-                if (__any((top - m[mt]) * a.scale > 8.f)) {
+                    for (int e = 0; e < 8; ++e) {
+                        pw[e] = pack_bf16(__builtin_amdgcn_exp2f(fmaf(x[mt][2 * e], a.scale, -off)), __builtin_amdgcn_exp2f(fmaf(x[mt][2 * e + 1], a.scale, -off)));
+                        part[e & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, pw[e]), one, part[e & 1], false);
+                    }
+                    sum = part[0] + part[1];
+                };
+                probabilities();
+                if (__any(sum > 1024.f)) {
+                    float top = x[mt][0];
+#pragma unroll
+                    for (int e = 1; e < 16; ++e) top = fmaxf(top, x[mt][e]);
                     const float up = fmaxf(m[mt], cross_group_max(top)), down = __builtin_amdgcn_exp2f((m[mt] - up) * a.scale);
                     m[mt] = up;
                     l[mt] *= down;
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) o[mt][dt] *= down;
+                    probabilities();
                 }
-                const float off = m[mt] * a.scale;
-                int pw[8];
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(x[mt][e], a.scale, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(x[mt][e + 1], a.scale, -off));
-                    l[mt] += p0 + p1;
-                    pw[e / 2] = pack_bf16(p0, p1);
-                }
+                l[mt] += sum;
                 pf[mt][0] = __builtin_bit_cast(v8bf, v4i{pw[0], pw[1], pw[2], pw[3]});
                 pf[mt][1] = __builtin_bit_cast(v8bf, v4i{pw[4], pw[5], pw[6], pw[7]});
             }
@@ -316,7 +346,7 @@ cache_attn_kernel(CacheAttnArgs a)
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[mt][e], o[mt][dt], 0, 0, 0);
                 }
-            if (j + W < last) load_v(j + W, page_v);
+            load_v(next, page_v, more);
         }
 
         // ---- the waves' sums, half of them at a time
@@ -505,12 +535,15 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
     a.row_tiles = (int)tiles;
     // the most steps that an item can have
     const int64_t reach = a.window ? std::min((int64_t)a.capacity, (int64_t)a.window + a.sinks + ROWS / a.G + 3 * STEP) : a.capacity;
+    const bool uni = a.c.page_shift >= 6;
     if (reach <= 20 * STEP)
-        return launch(cache_attn_kernel<D, E5M2, MT, 8, true>, dim3((unsigned)items), dim3(512), stream, a);
+        return uni ? launch(cache_attn_kernel<D, E5M2, MT, 8, true, true>, dim3((unsigned)items), dim3(512), stream, a)
+                   : launch(cache_attn_kernel<D, E5M2, MT, 8, true, false>, dim3((unsigned)items), dim3(512), stream, a);
     const int64_t grid = grid_of(MT);
     a.pieces = (float*)workspace;
     a.split = (int2*)(a.pieces + 2 * grid * ROWS * (D + 2));
-    const int rc = launch(cache_attn_kernel<D, E5M2, MT, 4, false>, dim3((unsigned)grid), dim3(256), stream, a);
+    const int rc = uni ? launch(cache_attn_kernel<D, E5M2, MT, 4, false, true>, dim3((unsigned)grid), dim3(256), stream, a)
+                       : launch(cache_attn_kernel<D, E5M2, MT, 4, false, false>, dim3((unsigned)grid), dim3(256), stream, a);
     if (rc != DMA_OK_) return rc;
     return launch(cache_attn_join_kernel<D, ROWS>, dim3((unsigned)items, (unsigned)std::min<int64_t>(ROWS / 4, ((int64_t)a.s.N * a.G + 3) / 4)), dim3(1024), stream, a);
 }

@@ -23,6 +23,13 @@ struct CacheAttnArgs {
     int2* split;             // ... per item: first and last workgroup that has a piece (first = last: no pieces)
 };
 
+// A word of a table that no kernel writes, at an index that is the same for all lanes: by way of the scalar cache, whose loads are counted
+// apart from those of the codes.
+DMA_DEV int scalar_at(const int* table, int index)
+{
+    return ((const __attribute__((address_space(4))) int*)(uintptr_t)table)[index];
+}
+
 struct SeqInfo {
     int start, n;
 };

@@ -61,11 +61,13 @@ cache_prompt_kernel(CacheAttnArgs a)
     // ---- codes of a step, from memory to registers and from there to LDS
     const int* table = c.page_table + (int64_t)b * c.max_pages;
     v4i kr[KCH], vr[VCH];
-    int kpage[UNI ? 1 : KCH], vpage[UNI ? 1 : VCH], ksc[UNI ? 1 : KCH], vsc[UNI ? 1 : VCH];
+    int kpage[UNI ? 1 : KCH], vpage[UNI ? 1 : VCH];
+    uint8_t ksc[UNI ? 1 : KCH], vsc[UNI ? 1 : VCH];
     bool vok[UNI ? 1 : VCH];
     auto page_at = [&](int p) -> int {
-        const int pi = p >> c.page_shift;
-        return pi < c.max_pages ? table[pi] : -1;
+        const int pi = p >> c.page_shift, at = min(pi, c.max_pages - 1);
+        const int page = UNI ? scalar_at(table, at) : table[at];
+        return pi < c.max_pages ? page : -1;
     };
     auto load_pages = [&](int j) {                                // one step before load(), two before stage()
         const int pos = range.position(j);
@@ -77,7 +79,7 @@ cache_prompt_kernel(CacheAttnArgs a)
             for (int u = 0; u < VCH; ++u) vpage[u] = page_at(pos + (threadIdx.x & 3) * 16);
         }
     };
-    const int kofs = threadIdx.x * 16, vofs = (threadIdx.x / 4 << c.page_shift) + (threadIdx.x & 3) * 16;
+    const unsigned kofs = threadIdx.x * 16, vofs = (threadIdx.x / 4 << c.page_shift) + (threadIdx.x & 3) * 16;
     auto load = [&](int j) {
         const int pos = range.position(j);
         if constexpr (UNI) {
