@@ -30,8 +30,8 @@ cache_attn_kernel(CacheAttnArgs a)
 {
     constexpr int ROWS = 16 * MT, KJ = D / 64, DT = D / 16, LD = D + 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
-    __shared__ float obuf[W / 2][ROWS][LD];
-    __shared__ float ml[W / 2][2][ROWS];
+    __shared__ __attribute__((aligned(16))) float obuf[W][ROWS][LD];
+    __shared__ float ml[W][2][ROWS];
     __shared__ int64_t scan[W + 1];
     const CacheView& c = a.c;
     const int page_mask = (1 << c.page_shift) - 1;
@@ -114,7 +114,7 @@ cache_attn_kernel(CacheAttnArgs a)
         }
         __syncthreads();
         b = found;
-        sq = seq_of(a, b);
+        sq = seq_of(a, b);                                      // (from the caches now)
         const int tiles = (int)(((int64_t)sq.n * a.G + ROWS - 1) / ROWS);
         int64_t per_head = 0;
         for (int i = 0; i < tiles; ++i) per_head += max(range_of<ROWS>(a, sq, i).steps, 1);
@@ -129,92 +129,137 @@ cache_attn_kernel(CacheAttnArgs a)
         skip = (int)at;
     }
 
-    // ---- item after item
+    // ---- item after item.  The codes of an item's first steps are requested before the sums of the one before it are joined.
+    StepRange range = {0, 0, 0};
+    int weight = 1, until = 0, rows = 0, all_hi = 0, all_lo = 0, last = 0, j = 0;
+    v8bf qf[MT][2 * KJ];
+    int vis_lo[MT], vis_hi[MT];              // what the row of this lane's column sees: these positions and those below sinks
+    const int* table = nullptr;
+    v4i kr[4][KJ], vr[DT];
+    uint8_t k_scale = 0, v_scale = 0;
+    int v_page = -1, pk = -1, pv = -1;       // pages of the step after the next
+    // Pages of a step: of the 16 positions whose keys this lane loads, and of those whose values it loads.
+    auto page_of = [&](int jj, int g) -> int {
+        const int pi = (range.position(jj) + (UNI ? 0 : 16 * g)) >> c.page_shift;
+        const int at = min(pi, c.max_pages - 1);
+        const int page = UNI ? scalar_at(table, __builtin_amdgcn_readfirstlane(at)) : table[at];
+        return pi < c.max_pages ? page : -1;
+    };
+    auto slab_of = [&](int page) -> int64_t {
+        if constexpr (UNI) page = __builtin_amdgcn_readfirstlane(page);
+        return (int64_t)((unsigned)page < c.page_limit ? page : 0) * c.Hkv + h;
+    };
+    // the positions of a lane's keys: 16 (col / 4) + 4 t + col % 4 in product t
+    auto load_k = [&](int jj, int page, bool on) {
+        const int64_t slab = slab_of(page);
+        const int pos = range.position(jj), at = 16 * (col >> 2);
+        const uint8_t* base = c.k_codes + ((slab << c.page_shift) + ((UNI ? pos : pos + at) & page_mask)) * D;
+        const uint8_t* p = base + (on ? (unsigned)(((UNI ? at : 0) + (col & 3)) * D + grp * 16) : 0u);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < KJ; ++i) kr[t][i] = *(const v4i*)(p + t * 4 * D + i * 64);
+        k_scale = c.k_scales[slab];
+    };
+    auto load_v = [&](int jj, int page, bool on) {
+        const int64_t slab = slab_of(page);
+        const int pos = range.position(jj);
+        const uint8_t* base = c.v_codes + ((slab * D) << c.page_shift) + ((UNI ? pos : pos + 16 * grp) & page_mask);
+        const unsigned mine = on ? (col << c.page_shift) + (UNI ? 16 * grp : 0) : 0u;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vr[dt] = *(const v4i*)(base + ((dt * 16) << c.page_shift) + mine);
+        v_scale = c.v_scales[slab];
+        v_page = page;
+    };
+
+    v4f o[MT][DT];
+    float m[MT], l[MT];
+    int old_b = 0, old_h = 0, old_tile = 0, old_rows = 0, old_piece = 0;      // the item whose sums are in o; its piece: -1: all of it
+    bool more = true;
     for (;;) {
-        const StepRange range = range_of<ROWS>(a, sq, tile);
-        const int weight = max(range.steps, 1);
-        const int until = BY_ITEM ? weight : (int)min((int64_t)weight, skip + left);
-        const int rows = (int)min((int64_t)sq.n * a.G - tile * ROWS, (int64_t)ROWS);
-        const int from = sq.start;
-
-        // the query rows of this lane's column, and what they see: positions [vis_lo, vis_hi] and those below sinks
-        v8bf qf[MT][2 * KJ];
-        int vis_lo[MT], vis_hi[MT];
+        if (more) {
+            range = range_of<ROWS>(a, sq, tile);
+            weight = max(range.steps, 1);
+            until = BY_ITEM ? weight : (int)min((int64_t)weight, skip + left);
+            rows = (int)min((int64_t)sq.n * a.G - tile * ROWS, (int64_t)ROWS);
+            last = min(until, range.steps);
+            j = skip + wave;
+            table = c.page_table + (int64_t)b * c.max_pages;
+            if (j < last) {
+                pk = page_of(j, col >> 2);
+                pv = UNI ? pk : page_of(j, grp);
+            }
+            const int64_t from = sq.start;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = r / a.G;
-            const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + r - i * a.G) * a.q.stride_head + i * a.q.stride_token;
+            for (int mt = 0; mt < MT; ++mt) {
+                const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = r / a.G;
+                const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + r - i * a.G) * a.q.stride_head + i * a.q.stride_token;
 #pragma unroll
-            for (int j = 0; j < KJ; ++j)
+                for (int jj = 0; jj < KJ; ++jj)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) qf[mt][2 * j + e] = *(const v8bf*)(qp + (j * 64 + grp * 16 + e * 8) * 2);
-            const int64_t p = (int64_t)from + i;
-            vis_hi[mt] = (int)min(p, (int64_t)POS_MAX);
-            vis_lo[mt] = a.window ? (int)min(max(p - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
+                    for (int e = 0; e < 2; ++e) qf[mt][2 * jj + e] = *(const v8bf*)(qp + (jj * 64 + grp * 16 + e * 8) * 2);
+                vis_hi[mt] = (int)min(from + i, (int64_t)POS_MAX);
+                vis_lo[mt] = a.window ? (int)min(max(from + i - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
+            }
+            // ... and what all of them see
+            all_hi = (int)min(from + tile * ROWS / a.G, (int64_t)POS_MAX);
+            all_lo = a.window ? (int)min(max(from + (tile * ROWS + rows - 1) / a.G - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
+            __builtin_amdgcn_sched_barrier(0);
+            if (j < last) {
+                load_k(j, pk, true);
+                load_v(j, pv, true);
+                pk = page_of(min(j + W, last - 1), col >> 2);
+                pv = UNI ? pk : page_of(min(j + W, last - 1), grp);
+            }
         }
-        // ... and what all of them see
-        const int all_hi = (int)min((int64_t)from + tile * ROWS / a.G, (int64_t)POS_MAX);
-        const int all_lo = a.window ? (int)min(max((int64_t)from + (tile * ROWS + rows - 1) / a.G - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
 
-        v4f o[MT][DT];
-        float m[MT], l[MT];
+        // ---- the sums of the waves: of the item before
+        if (old_rows) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const float sum = cross_group_sum(l[mt]);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) *(v4f*)&obuf[wave][mt * 16 + col][dt * 16 + grp * 4] = o[mt][dt];
+                if (grp == 0) {
+                    ml[wave][0][mt * 16 + col] = m[mt];
+                    ml[wave][1][mt * 16 + col] = sum;
+                }
+            }
+            __syncthreads();
+            for (int at = threadIdx.x; at < old_rows * (D / 4); at += 64 * W) {
+                const int rr = at / (D / 4), ch = at % (D / 4);
+                float up = M_NONE, sum = 0.f;
+                for (int w = 0; w < W; ++w) up = fmaxf(up, ml[w][0][rr]);
+                v4f x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const float f = __builtin_amdgcn_exp2f((ml[w][0][rr] - up) * a.scale);
+                    sum += ml[w][1][rr] * f;
+                    x += *(const v4f*)&obuf[w][rr][ch * 4] * f;
+                }
+                if (BY_ITEM || old_piece < 0) {
+                    const int r = old_tile * ROWS + rr, i = r / a.G;
+                    char* op = a.out.data + old_b * a.out.stride_batch + (old_h * a.G + r - i * a.G) * a.out.stride_head + i * a.out.stride_token;
+                    x *= sum == 0.f ? 0.f : 1.f / sum;
+                    *(v2i*)(op + ch * 8) = v2i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+                } else {
+                    float* p = a.pieces + (int64_t)old_piece * (ROWS * (D + 2));
+                    *(v4f*)(p + rr * D + ch * 4) = x;
+                    if (ch == 0) {
+                        p[ROWS * D + rr] = up;
+                        p[ROWS * D + ROWS + rr] = sum;
+                    }
+                }
+            }
+            if (!more) return;
+            __syncthreads();                                      // before the next item's sums
+        }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[mt][dt] = v4f{0.f, 0.f, 0.f, 0.f};
             m[mt] = M_NONE;
             l[mt] = 0.f;
-        }
-
-        __builtin_amdgcn_sched_barrier(0);
-        // Pages of a step: of the 16 positions whose keys this lane loads, and of those whose values it loads.
-        const int* table = c.page_table + (int64_t)b * c.max_pages;
-        auto page_of = [&](int j, int g) -> int {
-            const int pi = (range.position(j) + (UNI ? 0 : 16 * g)) >> c.page_shift;
-            const int at = min(pi, c.max_pages - 1);
-            const int page = UNI ? scalar_at(table, __builtin_amdgcn_readfirstlane(at)) : table[at];
-            return pi < c.max_pages ? page : -1;
-        };
-        auto slab_of = [&](int page) -> int64_t {
-            if constexpr (UNI) page = __builtin_amdgcn_readfirstlane(page);
-            return (int64_t)((unsigned)page < c.page_limit ? page : 0) * c.Hkv + h;
-        };
-        v4i kr[4][KJ], vr[DT];
-        uint8_t k_scale, v_scale;
-        int v_page;
-        // the positions of a lane's keys: 16 (col / 4) + 4 t + col % 4 in product t
-        auto load_k = [&](int j, int page, bool on) {
-            const int64_t slab = slab_of(page);
-            const int pos = range.position(j), at = 16 * (col >> 2);
-            const uint8_t* base = c.k_codes + ((slab << c.page_shift) + ((UNI ? pos : pos + at) & page_mask)) * D;
-            const uint8_t* p = base + (on ? (unsigned)(((UNI ? at : 0) + (col & 3)) * D + grp * 16) : 0u);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int jj = 0; jj < KJ; ++jj) kr[t][jj] = *(const v4i*)(p + t * 4 * D + jj * 64);
-            k_scale = c.k_scales[slab];
-        };
-        auto load_v = [&](int j, int page, bool on) {
-            const int64_t slab = slab_of(page);
-            const int pos = range.position(j);
-            const uint8_t* base = c.v_codes + ((slab * D) << c.page_shift) + ((UNI ? pos : pos + 16 * grp) & page_mask);
-            const unsigned mine = on ? (col << c.page_shift) + (UNI ? 16 * grp : 0) : 0u;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) vr[dt] = *(const v4i*)(base + ((dt * 16) << c.page_shift) + mine);
-            v_scale = c.v_scales[slab];
-            v_page = page;
-        };
-
-        const int last = min(until, range.steps);
-        int j = skip + wave;
-        int pk = -1, pv = -1;                                     // pages of the step after the next
-        if (j < last) {
-            pk = page_of(j, col >> 2);
-            pv = UNI ? pk : page_of(j, grp);
-            load_k(j, pk, true);
-            load_v(j, pv, true);
-            pk = page_of(min(j + W, last - 1), col >> 2);
-            pv = UNI ? pk : page_of(min(j + W, last - 1), grp);
         }
         // the queries, requested first, have arrived before the loop: no wait for them inside it, which would be one for the codes
 #pragma unroll
@@ -349,82 +394,32 @@ cache_attn_kernel(CacheAttnArgs a)
             load_v(next, page_v, more);
         }
 
-        // ---- the waves' sums, half of them at a time
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) l[mt] = cross_group_sum(l[mt]);
-#pragma unroll
-        for (int half = W / 2; half; half >>= 1) {
-            if (wave >= half && wave < 2 * half) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) *(v4f*)&obuf[wave - half][mt * 16 + col][dt * 16 + grp * 4] = o[mt][dt];
-                    if (grp == 0) {
-                        ml[wave - half][0][mt * 16 + col] = m[mt];
-                        ml[wave - half][1][mt * 16 + col] = l[mt];
-                    }
-                }
-            }
-            __syncthreads();
-            if (wave < half) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const float m2 = ml[wave][0][mt * 16 + col], up = fmaxf(m[mt], m2);
-                    const float f1 = __builtin_amdgcn_exp2f((m[mt] - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2 - up) * a.scale);
-                    m[mt] = up;
-                    l[mt] = l[mt] * f1 + ml[wave][1][mt * 16 + col] * f2;
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        const v4f x = *(const v4f*)&obuf[wave][mt * 16 + col][dt * 16 + grp * 4];
-                        o[mt][dt] = o[mt][dt] * f1 + x * f2;
-                    }
-                }
-            }
-            __syncthreads();
-        }
-        const bool whole = BY_ITEM || (skip == 0 && until == weight);
-        if (wave == 0) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const int rr = mt * 16 + col;
-                if (rr >= rows) continue;
-                if (whole) {
-                    const int r = tile * ROWS + rr, i = r / a.G;
-                    char* op = a.out.data + b * a.out.stride_batch + (h * a.G + r - i * a.G) * a.out.stride_head + i * a.out.stride_token;
-                    const float inv = l[mt] == 0.f ? 0.f : 1.f / l[mt];
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        const v4f x = o[mt][dt] * inv;
-                        *(v2i*)(op + (dt * 16 + grp * 4) * 2) = v2i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-                    }
-                } else {
-                    float* p = a.pieces + (int64_t)(2 * wg + (skip == 0)) * (ROWS * (D + 2));
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) *(v4f*)(p + rr * D + dt * 16 + grp * 4) = o[mt][dt];
-                    if (grp == 0) {
-                        p[ROWS * D + rr] = m[mt];
-                        p[ROWS * D + ROWS + rr] = l[mt];
-                    }
-                }
-            }
-            if (!BY_ITEM && lane == 0) {
-                int* sp = (int*)(a.split + ((int64_t)b * c.Hkv + h) * a.row_tiles + tile);
-                if (skip == 0) sp[0] = wg;                         // the first piece's workgroup says so ...
-                if (until == weight) sp[1] = wg;                   // ... and the last one's
-            }
-        }
-        if constexpr (BY_ITEM) return;
+        // ---- what was worked on, and what comes next
+        old_b = b;
+        old_h = h;
+        old_tile = tile;
+        old_rows = rows;
+        if constexpr (BY_ITEM) more = false;
         else {
+            const bool first = skip == 0, ends = until == weight;
+            old_piece = first && ends ? -1 : 2 * wg + first;
+            if (threadIdx.x == 0) {
+                int* sp = (int*)(a.split + ((int64_t)b * c.Hkv + h) * a.row_tiles + tile);
+                if (first) sp[0] = wg;                             // the first piece's workgroup says so ...
+                if (ends) sp[1] = wg;                              // ... and the last one's
+            }
             left -= until - skip;
-            if (left <= 0) return;
             skip = 0;
-            ++tile;
-            while ((int64_t)tile * ROWS >= (int64_t)sq.n * a.G) {
-                tile = 0;
-                if (h + 1 < c.Hkv && sq.n > 0) ++h;
-                else {
-                    h = 0;
-                    sq = seq_of(a, ++b);
+            more = left > 0;
+            if (more) {
+                ++tile;
+                while ((int64_t)tile * ROWS >= (int64_t)sq.n * a.G) {
+                    tile = 0;
+                    if (h + 1 < c.Hkv && sq.n > 0) ++h;
+                    else {
+                        h = 0;
+                        sq = seq_of(a, ++b);
+                    }
                 }
             }
         }
