@@ -29,104 +29,108 @@ __global__ void __launch_bounds__(64 * W, 2)
 cache_attn_kernel(CacheAttnArgs a)
 {
     constexpr int ROWS = 16 * MT, KJ = D / 64, DT = D / 16, LD = D + 4;
+    constexpr bool ONE = MT == 1;            // a sequence's rows are one tile
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
     __shared__ __attribute__((aligned(16))) float obuf[W][ROWS][LD];
     __shared__ float ml[W][2][ROWS];
-    __shared__ int64_t scan[W + 1];
     const CacheView& c = a.c;
     const int page_mask = (1 << c.page_shift) - 1;
 
-    // ---- where this workgroup's share lies
-    int64_t begin = 0, left = 1;             // in steps; of the line
+    // ---- where this workgroup's share lies: every wave finds it by itself, 256 sequences at a time
+    int left = 1;                            // units of the share that are left
     int b = 0, h = 0, tile = 0;
     SeqInfo sq;
     int skip = 0;                            // steps of the first item that belong to others
     int wg = 0;                              // place in the line
+    // units of an item
+    auto units_of = [&](const SeqInfo& q, int i) { return (max(range_of<ROWS, ONE>(a, q, i).steps, 1) + (1 << a.unit_shift) - 1) >> a.unit_shift; };
+    auto tiles_of = [&](const SeqInfo& q) { return ONE ? (q.n > 0) : (int)(((unsigned)q.n * (unsigned)a.G + ROWS - 1) / ROWS); };
     if constexpr (BY_ITEM) {
         unsigned i = blockIdx.x;
-        tile = i % (unsigned)a.row_tiles;
-        i /= (unsigned)a.row_tiles;
+        if constexpr (!ONE) {
+            tile = i % (unsigned)a.row_tiles;
+            i /= (unsigned)a.row_tiles;
+        }
         h = i % (unsigned)c.Hkv;
         b = i / (unsigned)c.Hkv;
         sq = seq_of(a, b);
-        if ((int64_t)tile * ROWS >= (int64_t)sq.n * a.G) return;
+        if (tile >= tiles_of(sq)) return;
     } else {
-        auto weight = [&](int bb) -> int64_t {                    // of one kv head of a sequence
-            if (bb >= a.s.B) return 0;
-            const SeqInfo q = seq_of(a, bb);
-            const int tiles = (int)(((int64_t)q.n * a.G + ROWS - 1) / ROWS);
-            int64_t t = 0;
-            for (int i = 0; i < tiles; ++i) t += max(range_of<ROWS>(a, q, i).steps, 1);
-            return t * c.Hkv;
-        };
-        auto inclusive = [&](int64_t x) {                         // over the workgroup; the total goes to scan[W]
+        SeqInfo q4[4];
+        int mine[4], upto[4];                // units of a kv head of a lane's sequence, and of it and those before it among the 64
+        auto load4 = [&](int first) {
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int64_t y = __shfl_up(x, o);
-                if (lane >= o) x += y;
+            for (int k = 0; k < 4; ++k) {
+                const int bb = first + 64 * k + lane;
+                q4[k] = seq_of(a, min(bb, a.s.B - 1));
+                if (bb >= a.s.B) q4[k].n = 0;
             }
-            __syncthreads();
-            if (lane == 63) scan[wave] = x;
-            __syncthreads();
-            int64_t before = 0, all = 0;
-            for (int w = 0; w < W; ++w) {
-                if (w < wave) before += scan[w];
-                all += scan[w];
+            int sum = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                mine[k] = 0;
+                upto[k] = 0;
+                if (first + 64 * k >= a.s.B) continue;                    // the same for all lanes
+                const int tiles = tiles_of(q4[k]);
+                for (int i = 0; i < tiles; ++i) mine[k] += units_of(q4[k], i);
+                int x = mine[k];
+                x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);       // row_shr:1, 2, 4, 8
+                x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+                x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+                x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+                x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);       // row_bcast:15, 31
+                x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+                upto[k] = x;
+                sum += __builtin_amdgcn_readlane(x, 63);
             }
-            if (threadIdx.x == 0) scan[W] = all;
-            __syncthreads();
-            return x + before;
+            return sum;
         };
-        int64_t total = 0, mine = 0, upto = 0;
-        const int chunks = (a.s.B + 64 * W - 1) / (64 * W);
-        for (int k = 0; k < chunks; ++k) {
-            mine = weight(k * 64 * W + threadIdx.x);
-            upto = inclusive(mine);
-            total += scan[W];
-        }
+        int total = 0;
+        for (int first = 0; first < a.s.B; first += 256) total += load4(first);
+        total *= c.Hkv;
         // one workgroup per CU instead of two where a share would be short: fewer pieces to join and fewer starts for the same
         // bytes per CU (one sequence of 32k, 8 kv heads: 23.2 us with 512 shares of 8 steps, 21.7 with 256 of 16; 7 of 0.6k-3k,
         // 32 heads: 27.9 with 512 of 14, 30.9 with 420 of 16)
-        int64_t share = (total + gridDim.x - 1) / gridDim.x;
-        if (share < 10) share = max((total + gridDim.x / 2 - 1) / (gridDim.x / 2), (int64_t)MIN_SHARE);
+        int share = (int)(((unsigned)total + gridDim.x - 1) / gridDim.x);
+        if (share < 10) share = max((int)(((unsigned)total + gridDim.x / 2 - 1) / (gridDim.x / 2)), MIN_SHARE);
         // workgroups next to each other in the line on the same XCD (they are dealt out in turn): they may share a sequence's keys
-        const int shares = (int)((total + share - 1) / share), per = (shares + 7) / 8;
-        if ((int)(blockIdx.x / 8) >= per) return;
+        const int shares = (int)(((unsigned)total + share - 1) / (unsigned)share), per = (shares + 7) / 8;
         wg = blockIdx.x % 8 * per + blockIdx.x / 8;
-        begin = share * wg;
-        if (begin >= total) return;
-        left = min(share, total - begin);
-        // the sequence that holds `begin`
-        __shared__ int found;
-        __shared__ int64_t found_at;
-        int64_t base = 0;
-        for (int k = 0; k < chunks; ++k) {
-            if (chunks > 1) {
-                mine = weight(k * 64 * W + threadIdx.x);
-                upto = inclusive(mine);
+        if ((int)(blockIdx.x / 8) >= per || wg >= shares) return;
+        int at = share * wg;
+        left = min(share, total - at);
+        // the sequence that holds the share's first unit
+        for (int first = 0;; first += 256) {
+            if (a.s.B > 256) load4(first);                                // (few: they are in the registers)
+            bool found = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (found || first + 64 * k >= a.s.B) continue;
+                const int all = __builtin_amdgcn_readlane(upto[k], 63) * c.Hkv;
+                if (at < all) {
+                    const int who = __builtin_ctzll(__ballot(upto[k] * c.Hkv > at));
+                    b = first + 64 * k + who;
+                    sq.start = __builtin_amdgcn_readlane(q4[k].start, who);
+                    sq.n = __builtin_amdgcn_readlane(q4[k].n, who);
+                    const int per_head = __builtin_amdgcn_readlane(mine[k], who);
+                    at -= (__builtin_amdgcn_readlane(upto[k], who) - per_head) * c.Hkv;
+                    h = (int)((unsigned)at / (unsigned)per_head);
+                    at -= h * per_head;
+                    found = true;
+                } else {
+                    at -= all;
+                }
             }
-            if (begin >= base + upto - mine && begin < base + upto) {
-                found = k * 64 * W + threadIdx.x;
-                found_at = begin - (base + upto - mine);
+            if (found) break;
+        }
+        if constexpr (!ONE) {
+            for (;; ++tile) {
+                const int w = units_of(sq, tile);
+                if (at < w) break;
+                at -= w;
             }
-            base += scan[W];
-            if (begin < base) break;
         }
-        __syncthreads();
-        b = found;
-        sq = seq_of(a, b);                                      // (from the caches now)
-        const int tiles = (int)(((int64_t)sq.n * a.G + ROWS - 1) / ROWS);
-        int64_t per_head = 0;
-        for (int i = 0; i < tiles; ++i) per_head += max(range_of<ROWS>(a, sq, i).steps, 1);
-        int64_t at = found_at;
-        h = (int)(at / per_head);
-        at -= h * per_head;
-        for (;; ++tile) {
-            const int w = max(range_of<ROWS>(a, sq, tile).steps, 1);
-            if (at < w) break;
-            at -= w;
-        }
-        skip = (int)at;
+        skip = at << a.unit_shift;
     }
 
     // ---- item after item.  The codes of an item's first steps are requested before the sums of the one before it are joined.
@@ -178,10 +182,10 @@ cache_attn_kernel(CacheAttnArgs a)
     bool more = true;
     for (;;) {
         if (more) {
-            range = range_of<ROWS>(a, sq, tile);
+            range = range_of<ROWS, ONE>(a, sq, tile);
             weight = max(range.steps, 1);
-            until = BY_ITEM ? weight : (int)min((int64_t)weight, skip + left);
-            rows = (int)min((int64_t)sq.n * a.G - tile * ROWS, (int64_t)ROWS);
+            until = BY_ITEM ? weight : (int)min((int64_t)weight, skip + ((int64_t)left << a.unit_shift));
+            rows = min(sq.n * a.G - tile * ROWS, ROWS);
             last = min(until, range.steps);
             j = skip + wave;
             table = c.page_table + (int64_t)b * c.max_pages;
@@ -192,7 +196,7 @@ cache_attn_kernel(CacheAttnArgs a)
             const int64_t from = sq.start;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = r / a.G;
+                const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = token_of<ONE>(a, r);
                 const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + r - i * a.G) * a.q.stride_head + i * a.q.stride_token;
 #pragma unroll
                 for (int jj = 0; jj < KJ; ++jj)
@@ -202,8 +206,8 @@ cache_attn_kernel(CacheAttnArgs a)
                 vis_lo[mt] = a.window ? (int)min(max(from + i - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
             }
             // ... and what all of them see
-            all_hi = (int)min(from + tile * ROWS / a.G, (int64_t)POS_MAX);
-            all_lo = a.window ? (int)min(max(from + (tile * ROWS + rows - 1) / a.G - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
+            all_hi = (int)min(from + (ONE ? 0 : tile * ROWS / a.G), (int64_t)POS_MAX);
+            all_lo = a.window ? (int)min(max(from + token_of<ONE>(a, tile * ROWS + rows - 1) - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
             __builtin_amdgcn_sched_barrier(0);
             if (j < last) {
                 load_k(j, pk, true);
@@ -238,7 +242,7 @@ cache_attn_kernel(CacheAttnArgs a)
                     x += *(const v4f*)&obuf[w][rr][ch * 4] * f;
                 }
                 if (BY_ITEM || old_piece < 0) {
-                    const int r = old_tile * ROWS + rr, i = r / a.G;
+                    const int r = old_tile * ROWS + rr, i = token_of<ONE>(a, r);
                     char* op = a.out.data + old_b * a.out.stride_batch + (old_h * a.G + r - i * a.G) * a.out.stride_head + i * a.out.stride_token;
                     x *= sum == 0.f ? 0.f : 1.f / sum;
                     *(v2i*)(op + ch * 8) = v2i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -408,12 +412,12 @@ cache_attn_kernel(CacheAttnArgs a)
                 if (first) sp[0] = wg;                             // the first piece's workgroup says so ...
                 if (ends) sp[1] = wg;                              // ... and the last one's
             }
-            left -= until - skip;
+            left -= (until - skip + (1 << a.unit_shift) - 1) >> a.unit_shift;
             skip = 0;
             more = left > 0;
             if (more) {
                 ++tile;
-                while ((int64_t)tile * ROWS >= (int64_t)sq.n * a.G) {
+                while (tile >= tiles_of(sq)) {
                     tile = 0;
                     if (h + 1 < c.Hkv && sq.n > 0) ++h;
                     else {
@@ -534,6 +538,8 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
     if (reach <= 20 * STEP)
         return uni ? launch(cache_attn_kernel<D, E5M2, MT, 8, true, true>, dim3((unsigned)items), dim3(512), stream, a)
                    : launch(cache_attn_kernel<D, E5M2, MT, 8, true, false>, dim3((unsigned)items), dim3(512), stream, a);
+    // the units of the line are counted in 31 bits
+    while (items * ((a.capacity / STEP >> a.unit_shift) + 2) > 0x7fffffff) ++a.unit_shift;
     const int64_t grid = grid_of(MT);
     a.pieces = (float*)workspace;
     a.split = (int2*)(a.pieces + 2 * grid * ROWS * (D + 2));
@@ -552,6 +558,7 @@ int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const 
     a.out = out;
     a.s = s;
     a.G = Hq / c.Hkv;
+    a.inv_g = (65536u + a.G - 1) / a.G;
     a.window = window;
     a.sinks = window ? sinks : 0;
     a.capacity = c.num_pages ? c.max_pages << c.page_shift : 0;

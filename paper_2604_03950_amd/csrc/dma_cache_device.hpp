@@ -15,6 +15,8 @@ struct CacheAttnArgs {
     Rows q, out;
     Spans s;
     int G;                   // query heads per kv head
+    unsigned inv_g;          // ceil(2^16 / G)
+    int unit_shift;          // few rows: the line of all items' steps is cut in units of 1 << unit_shift of them
     int row_tiles;           // of a sequence with N tokens
     int window, sinks;
     int capacity;            // positions that a reader may find
@@ -42,15 +44,19 @@ DMA_DEV SeqInfo seq_of(const CacheAttnArgs& a, int b)
     return q;
 }
 
-// The steps that a row tile visits: [0, sink_steps) and [first, first + steps - sink_steps).
+// Token of a query row, counted from the row tile's first: a multiplication where the rows of a sequence are few (exact below 2^12 rows).
+template <bool FEW>
+DMA_DEV int token_of(const CacheAttnArgs& a, int row) { return FEW ? (int)((unsigned)row * a.inv_g >> 16) : row / a.G; }
+
+// The steps that a row tile visits: [0, sink_steps) and [first, first + steps - sink_steps).  ONE: a sequence has one tile.
 struct StepRange {
     int sink_steps, first, steps;
     DMA_DEV int position(int j) const { return (j < sink_steps ? j : first + j - sink_steps) * STEP; }
 };
-template <int ROWS>
+template <int ROWS, bool ONE>
 DMA_DEV StepRange range_of(const CacheAttnArgs& a, const SeqInfo& q, int tile)
 {
-    const int64_t from = (int64_t)q.start + tile * ROWS / a.G, to = (int64_t)q.start + min(q.n - 1, (tile * ROWS + ROWS - 1) / a.G);
+    const int64_t from = (int64_t)q.start + (ONE ? 0 : tile * ROWS / a.G), to = (int64_t)q.start + (ONE ? q.n - 1 : min(q.n - 1, (tile * ROWS + ROWS - 1) / a.G));
     const int hi = (int)min(to + 1, (int64_t)a.capacity);
     const int lo = a.window ? (int)min(max(from - a.window + 1, (int64_t)0), (int64_t)hi) : 0;
     StepRange r;

@@ -34,7 +34,7 @@ cache_prompt_kernel(CacheAttnArgs a)
     const SeqInfo sq = seq_of(a, b);
     const int rows = (int)min((int64_t)sq.n * a.G - (int64_t)tile * ROWS, (int64_t)ROWS);
     if (rows <= 0) return;
-    const StepRange range = range_of<ROWS>(a, sq, tile);
+    const StepRange range = range_of<ROWS, false>(a, sq, tile);
 
     // ---- rows of this wave
     const int r0 = tile * ROWS + wave * 32, my_rows = min(rows - wave * 32, 32);      // (none: the wave only helps)

@@ -255,6 +255,23 @@ def test_long_and_short_sequences_together(N, G, D, window):
     pair.attn(bf16(rng, B, G, N, D), start, np.zeros(B, int), window, 3)       # nothing at all
 
 
+@pytest.mark.parametrize("N", [1, 9])
+def test_table_of_the_largest_capacity(N):
+    """2^30 - 256 positions per sequence, more than 2^31 steps of work by the sizes alone: short sequences among -1 entries."""
+    rng = np.random.default_rng(N)
+    B, Hkv, P, D, wide = 64, 4, 256, 64, (1 << 22) - 1
+    lens = rng.integers(N, 700, B)
+    table, pages = table_of(rng, lens, P, spare=0)
+    pair = Pair(rng, None, Hkv, P, D, "e4m3", table, pages)
+    big = torch.full((B, wide), -1, dtype=torch.int32, device="cuda")
+    big[:, :table.shape[1]] = pair.gpu.page_table
+    pair.gpu = dma.KVCache(pair.gpu.k_codes, pair.gpu.v_codes, pair.gpu.k_scales, pair.gpu.v_scales, big)
+    n = int(max(lens))
+    pair.write(bf16(rng, B, Hkv, n, D), bf16(rng, B, Hkv, n, D), [0] * B, lens)
+    pair.same()
+    pair.attn(bf16(rng, B, Hkv * 2, N, D), lens - N)
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
 @pytest.mark.parametrize("B,Hkv,G,N", [(2, 1, 4, 3), (2, 1, 2, 20), (17, 4, 2, 100)])
 def test_nan_reaches_only_who_sees_it(fmt, B, Hkv, G, N):
