@@ -28,6 +28,8 @@ cache_prompt_kernel(CacheAttnArgs a)
 
     // the last tiles of a sequence have the most keys: first
     unsigned item = blockIdx.x;
+    const int part = item % (unsigned)a.parts;
+    item /= (unsigned)a.parts;
     const int h = item % (unsigned)c.Hkv;
     item /= (unsigned)c.Hkv;
     const int b = item % (unsigned)a.s.B, tile = a.row_tiles - 1 - (int)(item / (unsigned)a.s.B);
@@ -35,6 +37,10 @@ cache_prompt_kernel(CacheAttnArgs a)
     const int rows = (int)min((int64_t)sq.n * a.G - (int64_t)tile * ROWS, (int64_t)ROWS);
     if (rows <= 0) return;
     const StepRange range = range_of<ROWS, false>(a, sq, tile);
+    // the steps of this piece
+    const int parts = parts_of(range.steps, a.parts);
+    if (part >= parts) return;
+    const int begin = (int)((int64_t)range.steps * part / parts), end = (int)((int64_t)range.steps * (part + 1) / parts);
 
     // ---- rows of this wave
     const int r0 = tile * ROWS + wave * 32, my_rows = min(rows - wave * 32, 32);      // (none: the wave only helps)
@@ -161,16 +167,16 @@ cache_prompt_kernel(CacheAttnArgs a)
     float m = M_NONE, l = 0.f;
 
     if (threadIdx.x < 4) odd_in[threadIdx.x] = 0;
-    if (range.steps > 0) {
-        load_pages(0);
-        load(0);
-        if (range.steps > 1) load_pages(1);
+    if (begin < end) {
+        load_pages(begin);
+        load(begin);
+        if (begin + 1 < end) load_pages(begin + 1);
     }
     __syncthreads();
-    if (range.steps > 0) {
-        stage(0, 0);
-        if (range.steps > 1) load(1);
-        if (range.steps > 2) load_pages(2);
+    if (begin < end) {
+        stage(begin, begin & 1);
+        if (begin + 1 < end) load(begin + 1);
+        if (begin + 2 < end) load_pages(begin + 2);
     }
     __syncthreads();
     // S rows of lane half `half`: register 4 q + i is row 8 q + 4 half + i of the 32, and holds position 16 (q / 2) + 8 half + 4 (q & 1) + i
@@ -182,12 +188,12 @@ cache_prompt_kernel(CacheAttnArgs a)
         asm volatile("" : "+v"(w));
         qf[ks] = __builtin_bit_cast(v8bf, w);
     }
-    for (int j = 0; j < range.steps; ++j) {
+    for (int j = begin; j < end; ++j) {
         const int buf = j & 1, pos = range.position(j);
-        if (j + 1 < range.steps) {
+        if (j + 1 < end) {
             stage(j + 1, buf ^ 1);
-            if (j + 2 < range.steps) load(j + 2);
-            if (j + 3 < range.steps) load_pages(j + 3);
+            if (j + 2 < end) load(j + 2);
+            if (j + 3 < end) load_pages(j + 3);
         }
         if (threadIdx.x == 0) odd_in[(j + 2) & 3] = 0;            // last read two steps ago, next written in the next one
         const int odd = odd_in[j & 3];
@@ -303,6 +309,21 @@ cache_prompt_kernel(CacheAttnArgs a)
 
     if (col >= my_rows) return;
     l = cross_half_sum(l);
+    if (parts > 1) {
+        const unsigned index = ((unsigned)b * c.Hkv + h) * a.row_tiles + tile;
+        float* p = a.pieces + ((int64_t)index * a.parts + part) * (ROWS * (D + 2));
+        const int rr = wave * 32 + col;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(v4f*)(p + rr * D + dt * 32 + 8 * q + 4 * half) = v4f{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]};
+        if (half == 0) {
+            p[ROWS * D + rr] = m;
+            p[ROWS * D + ROWS + rr] = l;
+        }
+        return;
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     char* op = a.out.data + b * a.out.stride_batch + (h * a.G + row - tok * a.G) * a.out.stride_head + tok * a.out.stride_token;
 #pragma unroll
@@ -312,16 +333,36 @@ cache_prompt_kernel(CacheAttnArgs a)
             *(v2i*)(op + (dt * 32 + 8 * q + 4 * half) * 2) = v2i{pack_bf16(o[dt][4 * q] * inv, o[dt][4 * q + 1] * inv), pack_bf16(o[dt][4 * q + 2] * inv, o[dt][4 * q + 3] * inv)};
 }
 
-int launch_cache_prompt(CacheAttnArgs a, hipStream_t stream)
+constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
+static int64_t prompt_items(int B, int Hkv, int G, int N) { return (int64_t)B * Hkv * (((int64_t)N * G + PROMPT_ROWS - 1) / PROMPT_ROWS); }
+
+// Pieces per item: as many workgroups as the chip holds (two per CU), where there are fewer items.
+int prompt_parts(int B, int Hkv, int G, int N)
 {
-    constexpr int NW = 4;
-    const int64_t tiles = ((int64_t)a.s.N * a.G + 32 * NW - 1) / (32 * NW), items = (int64_t)a.s.B * a.c.Hkv * tiles;
-    if (items * 64 * NW > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
-    a.row_tiles = (int)tiles;
-    const dim3 grid((unsigned)items), block(64 * NW);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(32, 2 * cache_cus() / prompt_items(B, Hkv, G, N)));
+}
+
+size_t cache_prompt_workspace(int B, int Hkv, int G, int N, int D)
+{
+    const int parts = prompt_parts(B, Hkv, G, N);
+    return parts > 1 ? (size_t)(prompt_items(B, Hkv, G, N) * parts * PROMPT_ROWS * (D + 2) * 4) : 0;
+}
+
+int launch_cache_prompt(CacheAttnArgs a, void* workspace, hipStream_t stream)
+{
+    constexpr int NW = PROMPT_WAVES;
+    const int64_t items = prompt_items(a.s.B, a.c.Hkv, a.G, a.s.N);
+    a.row_tiles = (int)(items / a.s.B / a.c.Hkv);
+    a.parts = prompt_parts(a.s.B, a.c.Hkv, a.G, a.s.N);
+    a.pieces = (float*)workspace;
+    if (items * a.parts * 64 * NW > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
+    const dim3 grid((unsigned)(items * a.parts)), block(64 * NW);
     auto go = [&](auto D, auto E5M2) {
-        return a.c.page_shift >= 6 ? launch(cache_prompt_kernel<D, E5M2 != 0, NW, true>, grid, block, stream, a)
-                                   : launch(cache_prompt_kernel<D, E5M2 != 0, NW, false>, grid, block, stream, a);
+        int rc = a.c.page_shift >= 6 ? launch(cache_prompt_kernel<D, E5M2 != 0, NW, true>, grid, block, stream, a)
+                                     : launch(cache_prompt_kernel<D, E5M2 != 0, NW, false>, grid, block, stream, a);
+        if (rc == DMA_OK_ && a.parts > 1)
+            rc = launch(cache_attn_join_kernel<D, PROMPT_ROWS, true>, dim3((unsigned)items, PROMPT_ROWS / 4), dim3(1024), stream, a);
+        return rc;
     };
     if (a.c.D == 128) return a.c.e5m2 ? go(IC<128>{}, IC<1>{}) : go(IC<128>{}, IC<0>{});
     return a.c.e5m2 ? go(IC<64>{}, IC<1>{}) : go(IC<64>{}, IC<0>{});
