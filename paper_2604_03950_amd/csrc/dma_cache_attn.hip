@@ -448,8 +448,9 @@ int cache_cus()
 static int mt_of(int G, int N) { return (int64_t)G * N <= 16 ? 1 : 2; }
 static int64_t grid_of(int mt) { return (int64_t)cache_cus() * 2; }
 
-// Whether the kernel for many rows serves the call.
-static bool many_rows(int G, int N) { return (int64_t)N * G >= 128; }
+// Whether the kernel for many rows serves the call: where the other one would need more than two tiles of 32 rows (us with either, 16
+// sequences of 4k: 64 rows 52.9 and 56.7, 96 rows 86.7 and 63.3; D = 64, 64 sequences: 64 rows 103 and 98, 124 rows 191 and 115).
+static bool many_rows(int G, int N) { return (int64_t)N * G > 64; }
 
 size_t cache_attn_workspace(int B, int Hq, int Hkv, int N, int D)
 {
