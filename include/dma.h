@@ -259,8 +259,9 @@ int dma_kv_read(const dma_kv_cache* cache, const dma_rows* k_out, const dma_rows
 int dma_cache_attn(const dma_kv_cache* cache, const dma_rows* q, const dma_rows* out, int B, int Hq, int N, const void* start_i32,
                    const void* n_tokens_i32, int window, int sink_tokens, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace of a dma_cache_attn call of these sizes on the current device; 0 also for sizes that the call refuses. */
-size_t dma_cache_attn_workspace_bytes(int B, int Hq, int Hkv, int N, int D);
+/* Bytes of workspace of a dma_cache_attn call with these arguments on the current device (of the cache only the sizes are looked at);
+ * 0 also for arguments that the call refuses. */
+size_t dma_cache_attn_workspace_bytes(const dma_kv_cache* cache, int B, int Hq, int N, int window, int sink_tokens);
 
 /* Diagnostic, not part of the method: plain device-to-device copy kernel (16 bytes per lane, no reuse) of `bytes`
  * bytes (a multiple of 16; src, dst 16-byte aligned, device, non-overlapping).  Its exactly known traffic (bytes read +

@@ -82,7 +82,7 @@ def load() -> ctypes.CDLL:
         L.dma_cache_attn.restype = ci
         L.dma_cache_attn.argtypes = [pc, pr, pr, ci, ci, ci, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
         L.dma_cache_attn_workspace_bytes.restype = ctypes.c_size_t
-        L.dma_cache_attn_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+        L.dma_cache_attn_workspace_bytes.argtypes = [pc, ci, ci, ci, ci, ci]
         L.dma_diag_copy.restype = ci
         L.dma_diag_copy.argtypes = [vp, vp, i64, vp]
         L.dma_diag_mfma.restype = ci
@@ -258,12 +258,14 @@ class KVCache:
         pages, Hkv, P, D = k_codes.shape
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
         self.page_table, self.fmt, self.device = page_table, int(fmt), k_codes.device
+        self._index = k_codes.get_device()
         self.Hkv, self.D, self.page_tokens = Hkv, D, P
         self.B, max_pages = page_table.shape
+        self._b = (self.B,)
         self._c = _Cache(_dev(k_codes, torch.uint8, "k_codes"), _dev(v_codes, torch.uint8, "v_codes", (pages, Hkv, D, P)),
                          _dev(k_scales, torch.uint8, "k_scales", (pages, Hkv)), _dev(v_scales, torch.uint8, "v_scales", (pages, Hkv)),
                          _dev(page_table, torch.int32, "page_table"), pages, max_pages, P, Hkv, D, int(fmt))
-        if any(t.device != self.device for t in (v_codes, k_scales, v_scales, page_table)):
+        if any(t.get_device() != self._index for t in (v_codes, k_scales, v_scales, page_table)):
             raise ValueError("the tensors of a cache must be on one GPU")
         self._ref = ctypes.byref(self._c)
 
@@ -276,9 +278,12 @@ class KVCache:
                    page_table, fmt)
 
 
-def _rows(t: torch.Tensor, what: str, shape, device) -> _Rows:
+_BF16, _I32 = torch.bfloat16, torch.int32
+
+
+def _rows(t: torch.Tensor, what: str, shape, index: int) -> _Rows:
     """A bf16 tensor [B, heads, N, D] whose rows are dense, at any strides the library takes (it checks them)."""
-    if t.dtype != torch.bfloat16 or t.device != device or t.shape != shape:
+    if t.dtype is not _BF16 or t.get_device() != index or t.shape != shape:
         raise ValueError(f"{what}: need a torch.bfloat16 tensor {tuple(shape)} on the cache's GPU")
     sb, sh, sn, sd = t.stride()
     if sd != 1:
@@ -287,30 +292,32 @@ def _rows(t: torch.Tensor, what: str, shape, device) -> _Rows:
     return _Rows(t.data_ptr(), sb if shape[0] > 1 else 0, sh if shape[1] > 1 else 0, sn if shape[2] > 1 else 0)
 
 
-def _spans(cache: KVCache, start: torch.Tensor, n_tokens: torch.Tensor | None):
-    """Pointers of start and n_tokens.  The call goes to the current stream, which has to be one of the cache's GPU."""
-    device = cache.device
-    if device.index != (_current_device or torch.cuda.current_device)():
-        raise ValueError(f"the cache is on {device}, which is not the current device")
-    if start.device != device or start.shape != (cache.B,):
-        raise ValueError(f"start: need [{cache.B}] on the cache's GPU")
-    if n_tokens is None:
-        return _dev(start, torch.int32, "start"), None
-    if n_tokens.device != device:
-        raise ValueError("n_tokens: need it on the cache's GPU")
-    return _dev(start, torch.int32, "start"), _dev(n_tokens, torch.int32, "n_tokens", (cache.B,))
+def _counts(cache: KVCache, t: torch.Tensor, what: str) -> int:
+    if t.dtype is not _I32 or t.get_device() != cache._index or t.shape != cache._b or not t.is_contiguous():
+        raise ValueError(f"{what}: need a contiguous torch.int32 tensor [{cache.B}] on the cache's GPU")
+    return t.data_ptr()
+
+
+def _cache_stream(cache: KVCache) -> int:
+    """The current stream of the cache's GPU, which has to be the current one."""
+    index = cache._index
+    if index != (_current_device or torch.cuda.current_device)():
+        raise ValueError(f"the cache is on {cache.device}, which is not the current device")
+    return _stream() if _raw_stream is None else _raw_stream(index)
 
 
 def dma_kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor, n_tokens: torch.Tensor | None = None) -> None:
     """Quantizes k, v [B, Hkv, N, D] bf16 (any strides with dense rows) into the cache: token i of sequence b at position
     start[b] + i, the first n_tokens[b] of them (all by default); start, n_tokens: int32 [B] on the GPU."""
-    ps, pn = _spans(cache, start, n_tokens)
+    stream = _cache_stream(cache)
+    ps = _counts(cache, start, "start")
+    pn = None if n_tokens is None else _counts(cache, n_tokens, "n_tokens")
     if k.dim() != 4:
         raise ValueError("k must be [B, Hkv, N, D]")
-    N = k.shape[2]
-    shape = (cache.B, cache.Hkv, N, cache.D)
-    rk, rv = _rows(k, "k", shape, cache.device), _rows(v, "v", shape, cache.device)
-    rc = load().dma_kv_write(cache._ref, rk, rv, cache.B, N, ps, pn, _stream())
+    B, N, index = cache.B, k.shape[2], cache._index
+    shape = (B, cache.Hkv, N, cache.D)
+    rk, rv = _rows(k, "k", shape, index), _rows(v, "v", shape, index)
+    rc = load().dma_kv_write(cache._ref, rk, rv, B, N, ps, pn, stream)
     if rc:
         raise DmaError(rc, "dma_kv_write")
 
@@ -318,18 +325,21 @@ def dma_kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, start: torch.
 def dma_kv_read(cache: KVCache, start: torch.Tensor, N: int | None = None, n_tokens: torch.Tensor | None = None, out=None):
     """Reads positions start[b] + [0, n_tokens[b]) back: (k, v) [B, Hkv, N, D] bf16.  Rows that do not exist are left as they
     were in out = (k, v), whose token dimension then gives N; without out they are zeros."""
-    ps, pn = _spans(cache, start, n_tokens)
+    stream = _cache_stream(cache)
+    ps = _counts(cache, start, "start")
+    pn = None if n_tokens is None else _counts(cache, n_tokens, "n_tokens")
+    B, index = cache.B, cache._index
     if out is None:
         if N is None:
             raise ValueError("N or out is needed")
-        out = tuple(torch.zeros((cache.B, cache.Hkv, N, cache.D), dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+        out = tuple(torch.zeros((B, cache.Hkv, N, cache.D), dtype=_BF16, device=cache.device) for _ in range(2))
     k, v = out
     if k.dim() != 4 or (N is not None and k.shape[2] != N):
         raise ValueError("out must be two tensors [B, Hkv, N, D]")
     N = k.shape[2]
-    shape = (cache.B, cache.Hkv, N, cache.D)
-    rk, rv = _rows(k, "k", shape, cache.device), _rows(v, "v", shape, cache.device)
-    rc = load().dma_kv_read(cache._ref, rk, rv, cache.B, N, ps, pn, _stream())
+    shape = (B, cache.Hkv, N, cache.D)
+    rk, rv = _rows(k, "k", shape, index), _rows(v, "v", shape, index)
+    rc = load().dma_kv_read(cache._ref, rk, rv, B, N, ps, pn, stream)
     if rc:
         raise DmaError(rc, "dma_kv_read")
     return k, v
@@ -339,36 +349,41 @@ def dma_cache_attn(q: torch.Tensor, cache: KVCache, start: torch.Tensor, n_token
                    sink_tokens: int = 0, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """q [B, Hq, N, D] bf16 (any strides with dense rows), token i of sequence b at position start[b] + i, attends to the
     cache's keys at and before its own position (window > 0: to the last `window` of them and the first sink_tokens positions)
-    -> out [B, Hq, N, D] bf16.  Rows behind n_tokens are left as they were in out; without out they are zeros.
+    -> out [B, Hq, N, D] bf16.  Rows that do not exist (behind n_tokens, or of a sequence with a
+    negative start) are left as they were in out; without out they are zeros.
     workspace: contiguous uint8 of at least dma_cache_attn_workspace_bytes(...) bytes, for one call at a time; by default one
     is allocated."""
-    ps, pn = _spans(cache, start, n_tokens)
+    stream = _cache_stream(cache)
+    ps = _counts(cache, start, "start")
+    pn = None if n_tokens is None else _counts(cache, n_tokens, "n_tokens")
     if q.dim() != 4:
         raise ValueError("q must be [B, Hq, N, D]")
-    device = cache.device
+    B, index = cache.B, cache._index
     _, Hq, N, _ = q.shape
-    shape = (cache.B, Hq, N, cache.D)
-    rq = _rows(q, "q", shape, device)
+    shape = (B, Hq, N, cache.D)
+    rq = _rows(q, "q", shape, index)
     if out is None:
-        out = (torch.empty if n_tokens is None else torch.zeros)(shape, dtype=torch.bfloat16, device=device)
-    ro = _rows(out, "out", shape, device)
+        out = torch.zeros(shape, dtype=_BF16, device=cache.device)
+    ro = _rows(out, "out", shape, index)
     L = load()
     if workspace is None:
-        need = L.dma_cache_attn_workspace_bytes(cache.B, Hq, cache.Hkv, N, cache.D)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    elif workspace.device != device:
+        pw, nw = None, L.dma_cache_attn_workspace_bytes(cache._ref, B, Hq, N, window, sink_tokens)
+        if nw:
+            workspace = torch.empty(nw, dtype=torch.uint8, device=cache.device)
+            pw = workspace.data_ptr()
+    elif workspace.get_device() != index:
         raise ValueError("workspace: need it on the cache's GPU")
-    pw, nw = (None, 0) if workspace is None else (_dev(workspace, torch.uint8, "workspace"), workspace.numel())
-    rc = L.dma_cache_attn(cache._ref, rq, ro, cache.B, Hq, N, ps, pn, int(window), int(sink_tokens), pw, nw, _stream())
+    else:
+        pw, nw = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
+    rc = L.dma_cache_attn(cache._ref, rq, ro, B, Hq, N, ps, pn, window, sink_tokens, pw, nw, stream)
     if rc:
         raise DmaError(rc, "dma_cache_attn")
     return out
 
 
-def dma_cache_attn_workspace_bytes(B: int, Hq: int, Hkv: int, N: int, D: int) -> int:
-    """Bytes of workspace of a dma_cache_attn call of these sizes on the current device."""
-    return int(load().dma_cache_attn_workspace_bytes(B, Hq, Hkv, N, D))
+def dma_cache_attn_workspace_bytes(cache: KVCache, Hq: int, N: int, window: int = 0, sink_tokens: int = 0) -> int:
+    """Bytes of workspace of a dma_cache_attn call with q [B, Hq, N, D] on the current device."""
+    return int(load().dma_cache_attn_workspace_bytes(cache._ref, cache.B, Hq, N, window, sink_tokens))
 
 
 def dma_diag_copy(src: torch.Tensor, dst: torch.Tensor) -> None:

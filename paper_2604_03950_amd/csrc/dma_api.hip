@@ -22,8 +22,7 @@ int check_quant_common(const void* x, int64_t rows, int D)
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-// B == 0 or N == 0 is a no-op that never looks at the tensors' pointers (an empty tensor has none).
-int check_cache(const dma_kv_cache* cache, int B, int N, dma::CacheView& c)
+int check_cache_sizes(const dma_kv_cache* cache, int B, int N, dma::CacheView& c)
 {
     if (!cache || B < 0 || N < 0) return DMA_ERR_INVALID_ARG;
     if (cache->fmt != DMA_FMT_MXFP8_E4M3 && cache->fmt != DMA_FMT_MXFP8_E5M2) return valid_fmt(cache->fmt) ? DMA_ERR_UNSUPPORTED : DMA_ERR_INVALID_ARG;
@@ -33,6 +32,21 @@ int check_cache(const dma_kv_cache* cache, int B, int N, dma::CacheView& c)
     if (cache->D != 64 && cache->D != 128) return DMA_ERR_UNSUPPORTED;
     if ((int64_t)cache->max_pages * P >= (int64_t)1 << 30 || N >= 1 << 30) return DMA_ERR_UNSUPPORTED;
     if (cache->num_pages > (((int64_t)1 << 40) - 1) / P / cache->D / cache->Hkv) return DMA_ERR_UNSUPPORTED;
+    c.num_pages = cache->num_pages;
+    c.page_limit = (unsigned)(cache->num_pages < 0x7fffffff ? cache->num_pages : 0x80000000LL);
+    c.max_pages = cache->max_pages;
+    c.page_shift = __builtin_ctz((unsigned)P);
+    c.Hkv = cache->Hkv;
+    c.D = cache->D;
+    c.e5m2 = cache->fmt == DMA_FMT_MXFP8_E5M2;
+    return DMA_OK;
+}
+
+// B == 0 or N == 0 is a no-op that never looks at the tensors' pointers (an empty tensor has none).
+int check_cache(const dma_kv_cache* cache, int B, int N, dma::CacheView& c)
+{
+    const int rc = check_cache_sizes(cache, B, N, c);
+    if (rc != DMA_OK) return rc;
     if (B > 0 && N > 0) {
         if (cache->num_pages > 0 && (!cache->k_codes || !cache->v_codes || !cache->k_scales || !cache->v_scales)) return DMA_ERR_INVALID_ARG;
         if (cache->max_pages > 0 && !cache->page_table) return DMA_ERR_INVALID_ARG;
@@ -41,13 +55,6 @@ int check_cache(const dma_kv_cache* cache, int B, int N, dma::CacheView& c)
     c.k_codes = (uint8_t*)cache->k_codes; c.v_codes = (uint8_t*)cache->v_codes;
     c.k_scales = (uint8_t*)cache->k_scales; c.v_scales = (uint8_t*)cache->v_scales;
     c.page_table = (const int*)cache->page_table;
-    c.num_pages = cache->num_pages;
-    c.page_limit = (unsigned)(cache->num_pages < 0x7fffffff ? cache->num_pages : 0x80000000LL);
-    c.max_pages = cache->max_pages;
-    c.page_shift = __builtin_ctz((unsigned)P);
-    c.Hkv = cache->Hkv;
-    c.D = cache->D;
-    c.e5m2 = cache->fmt == DMA_FMT_MXFP8_E5M2;
     return DMA_OK;
 }
 
@@ -246,15 +253,16 @@ int dma_cache_attn(const dma_kv_cache* cache, const dma_rows* q, const dma_rows*
     if ((rc = check_spans(start_i32, n_tokens_i32, B, N, s)) != DMA_OK) return rc;
     if ((rc = check_rows(q, rq)) != DMA_OK || (rc = check_rows(out, ro)) != DMA_OK) return rc;
     if (!attn_sizes_fit(B, Hq, c.Hkv, N)) return DMA_ERR_UNSUPPORTED;
-    const size_t need = dma::cache_attn_workspace(B, Hq, c.Hkv, N, c.D);
+    const size_t need = dma::cache_attn_workspace(c, B, Hq, N, window, sink_tokens);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return DMA_ERR_INVALID_ARG;
     return dma::launch_cache_attn(c, rq, ro, s, Hq, window, sink_tokens, workspace, (hipStream_t)stream);
 }
 
-size_t dma_cache_attn_workspace_bytes(int B, int Hq, int Hkv, int N, int D)
+size_t dma_cache_attn_workspace_bytes(const dma_kv_cache* cache, int B, int Hq, int N, int window, int sink_tokens)
 {
-    if (B <= 0 || Hq <= 0 || Hkv <= 0 || N <= 0 || Hq % Hkv != 0 || (D != 64 && D != 128) || !attn_sizes_fit(B, Hq, Hkv, N)) return 0;
-    return dma::cache_attn_workspace(B, Hq, Hkv, N, D);
+    dma::CacheView c;
+    if (check_cache_sizes(cache, B, N, c) != DMA_OK || B == 0 || N == 0 || Hq <= 0 || Hq % c.Hkv != 0 || window < 0 || sink_tokens < 0) return 0;
+    return attn_sizes_fit(B, Hq, c.Hkv, N) ? dma::cache_attn_workspace(c, B, Hq, N, window, sink_tokens) : 0;
 }
 
 int dma_diag_copy(const void* src, void* dst, int64_t bytes, void* stream)

@@ -452,12 +452,24 @@ static int64_t grid_of(int mt) { return (int64_t)cache_cus() * 2; }
 // sequences of 4k: 64 rows 52.9 and 56.7, 96 rows 86.7 and 63.3; D = 64, 64 sequences: 64 rows 103 and 98, 124 rows 191 and 115).
 static bool many_rows(int G, int N) { return (int64_t)N * G > 64; }
 
-size_t cache_attn_workspace(int B, int Hq, int Hkv, int N, int D)
+// The most positions that a row tile can visit.
+static int64_t reach_of(const CacheView& c, int rows, int G, int window, int sinks)
 {
-    if (many_rows(Hq / Hkv, N)) return cache_prompt_workspace(B, Hkv, Hq / Hkv, N, D);
-    const int mt = mt_of(Hq / Hkv, N);
-    const int64_t tiles = ((int64_t)N * (Hq / Hkv) + 16 * mt - 1) / (16 * mt), items = (int64_t)B * Hkv * tiles;
-    return (size_t)(2 * grid_of(mt) * (16 * mt) * (D + 2) * 4 + items * 8);
+    const int64_t capacity = (int64_t)c.max_pages << c.page_shift;
+    return window ? std::min(capacity, (int64_t)window + std::min(sinks, 1 << 30) + rows / G + 3 * STEP) : capacity;
+}
+// One workgroup per item, eight waves of it, where no item is longer than this: a second kernel to join pieces costs more than the
+// chip's other CUs save (one sequence of 1000, 8 kv heads: 10.6 us as one kernel).
+constexpr int64_t SHORT_REACH = 20 * STEP;
+
+size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window, int sinks)
+{
+    const int G = Hq / c.Hkv;
+    if (many_rows(G, N)) return cache_prompt_workspace(B, c.Hkv, G, N, c.D);
+    const int mt = mt_of(G, N), rows = 16 * mt;
+    if (reach_of(c, rows, G, window, sinks) <= SHORT_REACH) return 0;
+    const int64_t tiles = ((int64_t)N * G + rows - 1) / rows, items = (int64_t)B * c.Hkv * tiles;
+    return (size_t)(2 * grid_of(mt) * rows * (c.D + 2) * 4 + items * 8);
 }
 
 template <int D, bool E5M2, int MT>
@@ -467,10 +479,8 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
     const int64_t tiles = ((int64_t)a.s.N * a.G + ROWS - 1) / ROWS, items = (int64_t)a.s.B * a.c.Hkv * tiles;
     if (items * (ROWS / 4) * 1024 > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
     a.row_tiles = (int)tiles;
-    // the most steps that an item can have
-    const int64_t reach = a.window ? std::min((int64_t)a.capacity, (int64_t)a.window + a.sinks + ROWS / a.G + 3 * STEP) : a.capacity;
     const bool uni = a.c.page_shift >= 6;
-    if (reach <= 20 * STEP)
+    if (reach_of(a.c, ROWS, a.G, a.window, a.sinks) <= SHORT_REACH)
         return uni ? launch(cache_attn_kernel<D, E5M2, MT, 8, true, true>, dim3((unsigned)items), dim3(512), stream, a)
                    : launch(cache_attn_kernel<D, E5M2, MT, 8, true, false>, dim3((unsigned)items), dim3(512), stream, a);
     // the units of the line are counted in 31 bits

@@ -86,6 +86,6 @@ int launch_kv_read(const CacheView& c, const Rows& k, const Rows& v, const Spans
 
 int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const Spans& s, int Hq, int window, int sinks,
                       void* workspace, hipStream_t stream);
-size_t cache_attn_workspace(int B, int Hq, int Hkv, int N, int D);
+size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window, int sinks);
 
 }  // namespace dma

@@ -76,13 +76,23 @@ def test_nothing_to_do(lib):
 
 
 def test_workspace(lib):
-    need = lib.dma_cache_attn_workspace_bytes(1, 4, 2, 3, 128)
-    assert need == dma.dma_cache_attn_workspace_bytes(1, 4, 2, 3, 128)
-    for sizes in ((0, 4, 2, 3, 128), (1, 3, 2, 3, 128), (1, 4, 0, 3, 128), (1, 4, 2, 0, 128), (1, 4, 2, 3, 96), (1 << 20, 4, 2, 1 << 10, 128)):
-        assert lib.dma_cache_attn_workspace_bytes(*sizes) == 0
-    if need:
-        for ws, n in ((None, 0), (FAKE, need - 1), (FAKE + 8, need), (None, need)):
-            assert calls(lib, ws=ws, ws_bytes=n)[2] == INVALID
+    f = lib.dma_cache_attn_workspace_bytes
+    long = cache(max_pages=1000)
+    for n in (3, 70):
+        need = f(long, 1, 4, n, 0, 0)
+        assert need > 0
+        for ws, size in ((None, 0), (FAKE, need - 1), (FAKE + 8, need), (None, need)):
+            assert calls(lib, long, N=n, ws=ws, ws_bytes=size)[2] == INVALID
+    assert f(cache(max_pages=1000, k_codes=None, v_codes=None, k_scales=None, v_scales=None, page_table=None), 1, 4, 3, 0, 0) == f(long, 1, 4, 3, 0, 0)
+    # nothing to join where no query can see much
+    assert f(cache(), 1, 4, 3, 0, 0) == 0 == f(long, 1, 4, 3, 100, 4) and f(long, 1, 4, 3, 100, (1 << 31) - 1) == need_of(f, long)
+    for args in ((None, 1, 4, 3, 0, 0), (long, 0, 4, 3, 0, 0), (long, 1, 3, 3, 0, 0), (long, 1, 4, 0, 0, 0), (long, 1, 4, 3, -1, 0), (long, 1, 4, 3, 0, -1),
+                 (cache(D=96), 1, 4, 3, 0, 0), (cache(fmt=0), 1, 4, 3, 0, 0), (long, 1 << 20, 4, 1 << 10, 0, 0)):
+        assert f(*args) == 0
+
+
+def need_of(f, c):
+    return f(c, 1, 4, 3, 0, 0)
 
 
 def test_binding_takes_gpu_tensors_only():
@@ -99,6 +109,9 @@ class Cuda(torch.Tensor):
     is_cuda = True
     device = torch.device("cuda", 0)
 
+    def get_device(self):
+        return 0
+
 
 def on_gpu(*shape, dtype=torch.bfloat16):
     return torch.zeros(shape, dtype=dtype).as_subclass(Cuda)
@@ -107,6 +120,7 @@ def on_gpu(*shape, dtype=torch.bfloat16):
 @pytest.fixture
 def handle(monkeypatch):
     monkeypatch.setattr(dma, "_current_device", lambda: 0)
+    monkeypatch.setattr(dma, "_raw_stream", lambda index: 0x1000 + index)
 
     class Never:
         def __getattr__(self, name):
