@@ -20,7 +20,7 @@
 
 namespace dma {
 
-constexpr int MIN_SHARE = 8;                 // steps: two for each wave
+constexpr int MIN_SHARE = 8;                 // steps (units): one or two for each wave
 
 // BY_ITEM: one workgroup per item.  Otherwise the items' steps in equal shares.
 // UNI: pages of 64 positions and more, so that a step lies in one: its page is the same for all lanes.
@@ -88,11 +88,11 @@ cache_attn_kernel(CacheAttnArgs a)
         int total = 0;
         for (int first = 0; first < a.s.B; first += 256) total += load4(first);
         total *= c.Hkv;
-        // one workgroup per CU instead of two where a share would be short: fewer pieces to join and fewer starts for the same
-        // bytes per CU (one sequence of 32k, 8 kv heads: 23.2 us with 512 shares of 8 steps, 21.7 with 256 of 16; 7 of 0.6k-3k,
-        // 32 heads: 27.9 with 512 of 14, 30.9 with 420 of 16)
+        // one workgroup of four waves per CU instead of two where a share would be short: fewer pieces and starts (7 sequences of 0.6k-3k, 32
+        // heads: 27.9 us with 512 shares of 14 steps, 30.9 with 420 of 16)
         int share = (int)(((unsigned)total + gridDim.x - 1) / gridDim.x);
-        if (share < 10) share = max((int)(((unsigned)total + gridDim.x / 2 - 1) / (gridDim.x / 2)), MIN_SHARE);
+        if (W == 4 && share < 10) share = (int)(((unsigned)total + gridDim.x / 2 - 1) / (gridDim.x / 2));
+        share = max(share, MIN_SHARE);
         // workgroups next to each other in the line on the same XCD (they are dealt out in turn): they may share a sequence's keys
         const int shares = (int)(((unsigned)total + share - 1) / (unsigned)share), per = (shares + 7) / 8;
         wg = blockIdx.x % 8 * per + blockIdx.x / 8;
@@ -446,11 +446,23 @@ int cache_cus()
 
 // Rows per workgroup: 16 where a kv head has no more, else 32.
 static int mt_of(int G, int N) { return (int64_t)G * N <= 16 ? 1 : 2; }
-static int64_t grid_of(int mt) { return (int64_t)cache_cus() * 2; }
+
+// Waves of a workgroup where the steps are cut in shares; the chip holds 8 / waves of them per CU.  Eight where items are few: half the starts
+// and pieces for the same bytes.  Four otherwise: the waves of a workgroup end an item together, so eight leave more of a CU idle at its
+// end.  us with four and with eight, 16 rows: one sequence of 8k (8 items) 15.3, 13.2; of 128k 56.0, 53.8; 16 of 4k (128 items) 32.0, 31.6;
+// 32 of 0.4k-4k (256 items) 37.1, 41.7; 64 of 16k (512 items) 358, 377; 32 rows: 16 of 4k x 16 tokens (256 items) 52.8, 49.1; 16 of 2k x 17 tokens, 32
+// kv heads (512 items) 70.5, 77.4.
+static int waves_of(int mt, int64_t items) { return items <= (mt == 1 ? cache_cus() / 2 : cache_cus()) ? 8 : 4; }
+static int64_t grid_of(int waves) { return (int64_t)cache_cus() * 8 / waves; }
 
 // Whether the kernel for many rows serves the call: where the other one would need more than two tiles of 32 rows (us with either, 16
-// sequences of 4k: 64 rows 52.9 and 56.7, 96 rows 86.7 and 63.3; D = 64, 64 sequences: 64 rows 103 and 98, 124 rows 191 and 115).
-static bool many_rows(int G, int N) { return (int64_t)N * G > 64; }
+// sequences of 4k: 64 rows 52.9 and 56.7, 96 rows 86.7 and 63.3; D = 64, 64 sequences: 64 rows 103 and 98, 124 rows 191 and 115), and at D = 128 with
+// 17 rows and more where every sequence and kv head finds a place on the chip (16 sequences of 2k, 32 kv heads: 17 rows 70.5 and 59.6, 64 rows 119 and 77).
+static bool many_rows(int B, int Hkv, int G, int N, int D)
+{
+    const int64_t rows = (int64_t)N * G;
+    return rows > 64 || (rows > 16 && D == 128 && (int64_t)B * Hkv >= 2 * cache_cus());
+}
 
 // The most positions that a row tile can visit.
 static int64_t reach_of(const CacheView& c, int rows, int G, int window, int sinks)
@@ -465,11 +477,11 @@ constexpr int64_t SHORT_REACH = 20 * STEP;
 size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window, int sinks)
 {
     const int G = Hq / c.Hkv;
-    if (many_rows(G, N)) return cache_prompt_workspace(B, c.Hkv, G, N, c.D);
+    if (many_rows(B, c.Hkv, G, N, c.D)) return cache_prompt_workspace(B, c.Hkv, G, N, c.D);
     const int mt = mt_of(G, N), rows = 16 * mt;
     if (reach_of(c, rows, G, window, sinks) <= SHORT_REACH) return 0;
     const int64_t tiles = ((int64_t)N * G + rows - 1) / rows, items = (int64_t)B * c.Hkv * tiles;
-    return (size_t)(2 * grid_of(mt) * rows * (c.D + 2) * 4 + items * 8);
+    return (size_t)(2 * grid_of(waves_of(mt, items)) * rows * (c.D + 2) * 4 + items * 8);
 }
 
 template <int D, bool E5M2, int MT>
@@ -485,11 +497,15 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
                    : launch(cache_attn_kernel<D, E5M2, MT, 8, true, false>, dim3((unsigned)items), dim3(512), stream, a);
     // the units of the line are counted in 31 bits
     while (items * ((a.capacity / STEP >> a.unit_shift) + 2) > 0x7fffffff) ++a.unit_shift;
-    const int64_t grid = grid_of(MT);
+    const int waves = waves_of(MT, items);
+    const int64_t grid = grid_of(waves);
     a.pieces = (float*)workspace;
     a.split = (int2*)(a.pieces + 2 * grid * ROWS * (D + 2));
-    const int rc = uni ? launch(cache_attn_kernel<D, E5M2, MT, 4, false, true>, dim3((unsigned)grid), dim3(256), stream, a)
-                       : launch(cache_attn_kernel<D, E5M2, MT, 4, false, false>, dim3((unsigned)grid), dim3(256), stream, a);
+    const dim3 g((unsigned)grid), block(64 * waves);
+    auto go = [&](auto W) {
+        return uni ? launch(cache_attn_kernel<D, E5M2, MT, W, false, true>, g, block, stream, a) : launch(cache_attn_kernel<D, E5M2, MT, W, false, false>, g, block, stream, a);
+    };
+    const int rc = waves == 8 ? go(IC<8>{}) : go(IC<4>{});
     if (rc != DMA_OK_) return rc;
     return launch(cache_attn_join_kernel<D, ROWS, false>, dim3((unsigned)items, (unsigned)std::min<int64_t>(ROWS / 4, ((int64_t)a.s.N * a.G + 3) / 4)), dim3(1024), stream, a);
 }
@@ -508,7 +524,7 @@ int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const 
     a.sinks = window ? sinks : 0;
     a.capacity = c.num_pages ? c.max_pages << c.page_shift : 0;
     a.scale = (float)(1.4426950408889634074 / sqrt((double)c.D));
-    if (many_rows(a.G, s.N)) return launch_cache_prompt(a, workspace, stream);
+    if (many_rows(s.B, c.Hkv, a.G, s.N, c.D)) return launch_cache_prompt(a, workspace, stream);
     const int mt = mt_of(a.G, s.N);
     auto pick = [&](auto D, auto F) { return mt == 1 ? launch_few<D, F != 0, 1>(a, workspace, stream) : launch_few<D, F != 0, 2>(a, workspace, stream); };
     if (c.D == 128) return c.e5m2 ? pick(IC<128>{}, IC<1>{}) : pick(IC<128>{}, IC<0>{});
