@@ -430,6 +430,73 @@ cache_attn_kernel(CacheAttnArgs a)
     }
 }
 
+// Joins the pieces of split items: a workgroup per item and 4 of its rows; threads over channels (4 each), rows and pieces,
+// a thread's loads of several pieces in flight at a time.  Bound by latency: three dependent loads.
+template <int D, int ROWS>
+__global__ void __launch_bounds__(1024)
+cache_attn_join_kernel(CacheAttnArgs a)
+{
+    constexpr int CH = D / 4, PG = 1024 / (4 * CH), U = 4;
+    unsigned item = blockIdx.x;
+    const int tile = item % (unsigned)a.row_tiles;
+    const int h = item / (unsigned)a.row_tiles % (unsigned)a.c.Hkv, b = item / (unsigned)a.row_tiles / (unsigned)a.c.Hkv;
+    const int2 sp = a.split[item];                              // anything where the item does not exist
+    const SeqInfo sq = seq_of(a, b);
+    const int rows = (int)min((int64_t)sq.n * a.G - (int64_t)tile * ROWS, (int64_t)ROWS);
+    const int rr = blockIdx.y * 4 + threadIdx.x / CH % 4, ch = threadIdx.x % CH, pg = threadIdx.x / (4 * CH);
+    if ((int)blockIdx.y * 4 >= rows || sp.x == sp.y) return;
+    __shared__ v4f os[PG][4][CH];
+    __shared__ float ms[PG][4], ls[PG][4];
+    v4f o = {0.f, 0.f, 0.f, 0.f};
+    float m = M_NONE, l = 0.f;
+    const int r0 = min(rr, rows - 1);
+    for (int w = sp.x + pg; w <= sp.y; w += PG * U) {
+        float m2[U], l2[U];
+        v4f x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int wu = w + u * PG;
+            m2[u] = M_NONE;
+            l2[u] = 0.f;
+            x[u] = v4f{0.f, 0.f, 0.f, 0.f};
+            if (wu <= sp.y) {
+                const float* p = a.pieces + (int64_t)(2 * wu + (wu == sp.x)) * (ROWS * (D + 2));
+                m2[u] = p[ROWS * D + r0];
+                l2[u] = p[ROWS * D + ROWS + r0];
+                x[u] = *(const v4f*)(p + r0 * D + ch * 4);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (w + u * PG > sp.y) break;
+            const float up = fmaxf(m, m2[u]);
+            const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2[u] - up) * a.scale);
+            m = up;
+            l = l * f1 + l2[u] * f2;
+            o = o * f1 + x[u] * f2;
+        }
+    }
+    os[pg][rr & 3][ch] = o;
+    if (ch == 0) {
+        ms[pg][rr & 3] = m;
+        ls[pg][rr & 3] = l;
+    }
+    __syncthreads();
+    if (pg || rr >= rows) return;
+    const int groups = min(PG, sp.y - sp.x + 1);
+    for (int k = 1; k < groups; ++k) {
+        const float m2 = ms[k][rr & 3], up = fmaxf(m, m2);
+        const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2 - up) * a.scale);
+        m = up;
+        l = l * f1 + ls[k][rr & 3] * f2;
+        o = o * f1 + os[k][rr & 3][ch] * f2;
+    }
+    const int r = tile * ROWS + rr, i = r / a.G;
+    char* op = a.out.data + b * a.out.stride_batch + (h * a.G + r - i * a.G) * a.out.stride_head + i * a.out.stride_token;
+    const v4f x = o * (l == 0.f ? 0.f : 1.f / l);
+    *(v2i*)(op + ch * 8) = v2i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+}
+
 // ---------------------------------------------------------------------------------------------------------------- host
 int cache_cus()
 {
@@ -477,7 +544,7 @@ constexpr int64_t SHORT_REACH = 20 * STEP;
 size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window, int sinks)
 {
     const int G = Hq / c.Hkv;
-    if (many_rows(B, c.Hkv, G, N, c.D)) return cache_prompt_workspace(B, c.Hkv, G, N, c.D);
+    if (many_rows(B, c.Hkv, G, N, c.D)) return cache_prompt_workspace(B, c.Hkv, G, N, c.D, reach_of(c, 128, G, window, sinks));
     const int mt = mt_of(G, N), rows = 16 * mt;
     if (reach_of(c, rows, G, window, sinks) <= SHORT_REACH) return 0;
     const int64_t tiles = ((int64_t)N * G + rows - 1) / rows, items = (int64_t)B * c.Hkv * tiles;
@@ -507,7 +574,7 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
     };
     const int rc = waves == 8 ? go(IC<8>{}) : go(IC<4>{});
     if (rc != DMA_OK_) return rc;
-    return launch(cache_attn_join_kernel<D, ROWS, false>, dim3((unsigned)items, (unsigned)std::min<int64_t>(ROWS / 4, ((int64_t)a.s.N * a.G + 3) / 4)), dim3(1024), stream, a);
+    return launch(cache_attn_join_kernel<D, ROWS>, dim3((unsigned)items, (unsigned)std::min<int64_t>(ROWS / 4, ((int64_t)a.s.N * a.G + 3) / 4)), dim3(1024), stream, a);
 }
 
 int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const Spans& s, int Hq, int window, int sinks,
@@ -524,7 +591,7 @@ int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const 
     a.sinks = window ? sinks : 0;
     a.capacity = c.num_pages ? c.max_pages << c.page_shift : 0;
     a.scale = (float)(1.4426950408889634074 / sqrt((double)c.D));
-    if (many_rows(s.B, c.Hkv, a.G, s.N, c.D)) return launch_cache_prompt(a, workspace, stream);
+    if (many_rows(s.B, c.Hkv, a.G, s.N, c.D)) return launch_cache_prompt(a, reach_of(c, 128, a.G, window, a.sinks), workspace, stream);
     const int mt = mt_of(a.G, s.N);
     auto pick = [&](auto D, auto F) { return mt == 1 ? launch_few<D, F != 0, 1>(a, workspace, stream) : launch_few<D, F != 0, 2>(a, workspace, stream); };
     if (c.D == 128) return c.e5m2 ? pick(IC<128>{}, IC<1>{}) : pick(IC<128>{}, IC<0>{});

@@ -133,79 +133,13 @@ DMA_DEV unsigned long long nan_channels(const CacheAttnArgs& a, int b, int h, in
     return hit;
 }
 
-// Many query rows (dma_cache_prompt.hip): the steps of an item of 128 rows in `parts` pieces at most, of four steps at least.
-DMA_DEV int parts_of(int steps, int parts) { return max(min(parts, steps / 4), 1); }
-int prompt_parts(int B, int Hkv, int G, int N);
-size_t cache_prompt_workspace(int B, int Hkv, int G, int N, int D);
-int launch_cache_prompt(CacheAttnArgs a, void* workspace, hipStream_t stream);
+// Many query rows (dma_cache_prompt.hip): the steps of an item of 128 rows in `parts` pieces at most, of two steps at least.  reach: the most
+// positions that an item can visit.
+DMA_DEV int parts_of(int steps, int parts) { return max(min(parts, steps / 2), 1); }
+size_t cache_prompt_workspace(int B, int Hkv, int G, int N, int D, int64_t reach);
+int launch_cache_prompt(CacheAttnArgs a, int64_t reach, void* workspace, hipStream_t stream);
 
 // Compute units of the current device (256 where it cannot be asked).
 int cache_cus();
-
-// Joins the pieces of split items: a workgroup per item and 4 of its rows; threads over channels (4 each), rows and pieces,
-// a thread's loads of several pieces in flight at a time.  Bound by latency: three dependent loads.
-// PARTS: the pieces of an item lie side by side, a.parts of them at most; otherwise where a.split says.
-template <int D, int ROWS, bool PARTS>
-__global__ void __launch_bounds__(1024)
-cache_attn_join_kernel(CacheAttnArgs a)
-{
-    constexpr int CH = D / 4, PG = 1024 / (4 * CH), U = 4;
-    unsigned item = blockIdx.x;
-    const int tile = item % (unsigned)a.row_tiles;
-    const int h = item / (unsigned)a.row_tiles % (unsigned)a.c.Hkv, b = item / (unsigned)a.row_tiles / (unsigned)a.c.Hkv;
-    int2 sp = {0, 0};
-    if constexpr (!PARTS) sp = a.split[item];                   // anything where the item does not exist
-    const SeqInfo sq = seq_of(a, b);
-    const int rows = (int)min((int64_t)sq.n * a.G - (int64_t)tile * ROWS, (int64_t)ROWS);
-    const int rr = blockIdx.y * 4 + threadIdx.x / CH % 4, ch = threadIdx.x % CH, pg = threadIdx.x / (4 * CH);
-    if ((int)blockIdx.y * 4 >= rows) return;
-    if constexpr (PARTS) sp.y = parts_of(range_of<ROWS, false>(a, sq, tile).steps, a.parts) - 1;
-    if (sp.x == sp.y) return;
-    __shared__ v4f os[PG][4][CH];
-    __shared__ float ms[PG][4], ls[PG][4];
-    v4f o = {0.f, 0.f, 0.f, 0.f};
-    float m = M_NONE, l = 0.f;
-    const int r0 = min(rr, rows - 1);
-    for (int w = sp.x + pg; w <= sp.y; w += PG * U) {
-        float m2[U], l2[U];
-        v4f x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int wu = min(w + u * PG, sp.y);
-            const float* p = a.pieces + (PARTS ? (int64_t)item * a.parts + wu : (int64_t)(2 * wu + (wu == sp.x))) * (ROWS * (D + 2));
-            m2[u] = p[ROWS * D + r0];
-            l2[u] = p[ROWS * D + ROWS + r0];
-            x[u] = *(const v4f*)(p + r0 * D + ch * 4);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (w + u * PG > sp.y) break;
-            const float up = fmaxf(m, m2[u]);
-            const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2[u] - up) * a.scale);
-            m = up;
-            l = l * f1 + l2[u] * f2;
-            o = o * f1 + x[u] * f2;
-        }
-    }
-    os[pg][rr & 3][ch] = o;
-    if (ch == 0) {
-        ms[pg][rr & 3] = m;
-        ls[pg][rr & 3] = l;
-    }
-    __syncthreads();
-    if (pg || rr >= rows) return;
-    const int groups = min(PG, sp.y - sp.x + 1);
-    for (int k = 1; k < groups; ++k) {
-        const float m2 = ms[k][rr & 3], up = fmaxf(m, m2);
-        const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2 - up) * a.scale);
-        m = up;
-        l = l * f1 + ls[k][rr & 3] * f2;
-        o = o * f1 + os[k][rr & 3][ch] * f2;
-    }
-    const int r = tile * ROWS + rr, i = r / a.G;
-    char* op = a.out.data + b * a.out.stride_batch + (h * a.G + r - i * a.G) * a.out.stride_head + i * a.out.stride_token;
-    const v4f x = o * (l == 0.f ? 0.f : 1.f / l);
-    *(v2i*)(op + ch * 8) = v2i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-}
 
 }  // namespace dma

@@ -66,70 +66,74 @@ cache_prompt_kernel(CacheAttnArgs a)
 
     // ---- codes of a step, from memory to registers and from there to LDS
     const int* table = c.page_table + (int64_t)b * c.max_pages;
-    v4i kr[KCH], vr[VCH];
-    int kpage[UNI ? 1 : KCH], vpage[UNI ? 1 : VCH];
-    uint8_t ksc[UNI ? 1 : KCH], vsc[UNI ? 1 : VCH];
-    bool vok[UNI ? 1 : VCH];
+    struct Pages {
+        int k[UNI ? 1 : KCH], v[UNI ? 1 : VCH];
+    };
+    struct Codes {
+        v4i k[KCH], v[VCH];
+        uint8_t ksc[UNI ? 1 : KCH], vsc[UNI ? 1 : VCH];
+        bool there[UNI ? 1 : VCH];
+    };
     auto page_at = [&](int p) -> int {
         const int pi = p >> c.page_shift, at = min(pi, c.max_pages - 1);
         const int page = UNI ? scalar_at(table, at) : table[at];
         return pi < c.max_pages ? page : -1;
     };
-    auto load_pages = [&](int j) {                                // one step before load(), two before stage()
+    auto load_pages = [&](int j, Pages& pg) {                     // one step before load(), two before stage()
         const int pos = range.position(j);
-        if constexpr (UNI) kpage[0] = page_at(pos);
+        if constexpr (UNI) pg.k[0] = page_at(pos);
         else {
 #pragma unroll
-            for (int u = 0; u < KCH; ++u) kpage[u] = page_at(pos + (threadIdx.x + u * T) / (D / 16));
+            for (int u = 0; u < KCH; ++u) pg.k[u] = page_at(pos + (threadIdx.x + u * T) / (D / 16));
 #pragma unroll
-            for (int u = 0; u < VCH; ++u) vpage[u] = page_at(pos + (threadIdx.x & 3) * 16);
+            for (int u = 0; u < VCH; ++u) pg.v[u] = page_at(pos + (threadIdx.x & 3) * 16);
         }
     };
     const unsigned kofs = threadIdx.x * 16, vofs = (threadIdx.x / 4 << c.page_shift) + (threadIdx.x & 3) * 16;
-    auto load = [&](int j) {
+    auto load = [&](int j, const Pages& pg, Codes& cd) {
         const int pos = range.position(j);
         if constexpr (UNI) {
-            vok[0] = (unsigned)kpage[0] < c.page_limit;
-            const int64_t slab = (int64_t)(vok[0] ? kpage[0] : 0) * c.Hkv + h;
+            cd.there[0] = (unsigned)pg.k[0] < c.page_limit;
+            const int64_t slab = (int64_t)(cd.there[0] ? pg.k[0] : 0) * c.Hkv + h;
             const uint8_t* kb = c.k_codes + ((slab << c.page_shift) + (pos & page_mask)) * D;
             const uint8_t* vb = c.v_codes + ((slab * D) << c.page_shift) + (pos & page_mask);
 #pragma unroll
-            for (int u = 0; u < KCH; ++u) kr[u] = *(const v4i*)(kb + u * T * 16 + kofs);
+            for (int u = 0; u < KCH; ++u) cd.k[u] = *(const v4i*)(kb + u * T * 16 + kofs);
 #pragma unroll
-            for (int u = 0; u < VCH; ++u) vr[u] = *(const v4i*)(vb + ((u * T / 4) << c.page_shift) + vofs);
-            ksc[0] = c.k_scales[slab];
-            vsc[0] = c.v_scales[slab];
+            for (int u = 0; u < VCH; ++u) cd.v[u] = *(const v4i*)(vb + ((u * T / 4) << c.page_shift) + vofs);
+            cd.ksc[0] = c.k_scales[slab];
+            cd.vsc[0] = c.v_scales[slab];
         } else {
 #pragma unroll
             for (int u = 0; u < KCH; ++u) {
                 const int ch = threadIdx.x + u * T, p = pos + ch / (D / 16);
-                const int64_t slab = (int64_t)((unsigned)kpage[u] < c.page_limit ? kpage[u] : 0) * c.Hkv + h;
-                kr[u] = *(const v4i*)(c.k_codes + (((slab << c.page_shift) + (p & page_mask)) * D + ch % (D / 16) * 16));
-                ksc[u] = c.k_scales[slab];
+                const int64_t slab = (int64_t)((unsigned)pg.k[u] < c.page_limit ? pg.k[u] : 0) * c.Hkv + h;
+                cd.k[u] = *(const v4i*)(c.k_codes + (((slab << c.page_shift) + (p & page_mask)) * D + ch % (D / 16) * 16));
+                cd.ksc[u] = c.k_scales[slab];
             }
 #pragma unroll
             for (int u = 0; u < VCH; ++u) {
                 const int ch = threadIdx.x + u * T, p = pos + (ch & 3) * 16;
-                vok[u] = (unsigned)vpage[u] < c.page_limit;
-                const int64_t slab = (int64_t)(vok[u] ? vpage[u] : 0) * c.Hkv + h;
-                vr[u] = *(const v4i*)(c.v_codes + (((slab * D + ch / 4) << c.page_shift) + (p & page_mask)));
-                vsc[u] = c.v_scales[slab];
+                cd.there[u] = (unsigned)pg.v[u] < c.page_limit;
+                const int64_t slab = (int64_t)(cd.there[u] ? pg.v[u] : 0) * c.Hkv + h;
+                cd.v[u] = *(const v4i*)(c.v_codes + (((slab * D + ch / 4) << c.page_shift) + (p & page_mask)));
+                cd.vsc[u] = c.v_scales[slab];
             }
         }
     };
     // Rows of LDS are shifted in chunks of 16 bytes so that the 16 lanes of a read's turn find different banks (256 bytes of them: one
     // row, or two of 128 bytes): keys by the number of the lane that reads them, channels by theirs.
     auto shift_of = [](int lane_row, int row_bytes) { return row_bytes == 256 ? lane_row & 15 : lane_row >> 1 & 7; };
-    auto stage = [&](int j, int buf) {
+    auto stage = [&](int j, int buf, Codes& cd) {
         const int pos = range.position(j);
 #pragma unroll
         for (int u = 0; u < KCH; ++u) {
             const int ch = threadIdx.x + u * T, key = ch / (D / 16), d16 = ch % (D / 16);
             const int shift = shift_of((key & 3) | (key >> 1 & 4) | (key << 1 & 8), KROW);
-            const float sc = __int_as_float(ksc[UNI ? 0 : u] << 23);
+            const float sc = __int_as_float(cd.ksc[UNI ? 0 : u] << 23);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                *(v8bf*)(kbuf[buf] + key * KROW + ((2 * d16 + e) ^ shift) * 16) = decode8<E5M2>(kr[u][2 * e], kr[u][2 * e + 1], sc);
+                *(v8bf*)(kbuf[buf] + key * KROW + ((2 * d16 + e) ^ shift) * 16) = decode8<E5M2>(cd.k[u][2 * e], cd.k[u][2 * e + 1], sc);
         }
         // Where not all rows see all positions: values that no row sees may be anything, and a NaN among the others must not reach the
         // rows that do not see it through a probability of zero.  Zeros instead; NaN is put into the sums of those who see it below.
@@ -138,23 +142,23 @@ cache_prompt_kernel(CacheAttnArgs a)
 #pragma unroll
         for (int u = 0; u < VCH; ++u) {
             const int ch = threadIdx.x + u * T, d = ch / 4;
-            const float sc = __int_as_float(vsc[UNI ? 0 : u] << 23);
-            const bool there = vok[UNI ? 0 : u];
+            const float sc = __int_as_float(cd.vsc[UNI ? 0 : u] << 23);
+            const bool there = cd.there[UNI ? 0 : u];
             if (!there) odd |= 1 << (ch & 3);
             if (!open || !there) {
                 auto below = [&](int q) { return (1u << min(max(q - pos - (ch & 3) * 16, 0), 16)) - 1u; };
                 const unsigned seen = there ? below(any_hi + 1) & (~below(any_lo) | below(a.sinks)) : 0u;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    vr[u][w] &= bytes_of(seen >> (4 * w));
-                    const unsigned bad = no_number<E5M2>((unsigned)vr[u][w]);
+                    cd.v[u][w] &= bytes_of(seen >> (4 * w));
+                    const unsigned bad = no_number<E5M2>((unsigned)cd.v[u][w]);
                     if (bad) odd |= 16;
-                    vr[u][w] &= (int)~((bad >> 7) * 0xffu);
+                    cd.v[u][w] &= (int)~((bad >> 7) * 0xffu);
                 }
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                *(v8bf*)(vbuf[buf] + d * VROW + ((2 * (ch & 3) + e) ^ shift_of(d, VROW)) * 16) = decode8<E5M2>(vr[u][2 * e], vr[u][2 * e + 1], sc);
+                *(v8bf*)(vbuf[buf] + d * VROW + ((2 * (ch & 3) + e) ^ shift_of(d, VROW)) * 16) = decode8<E5M2>(cd.v[u][2 * e], cd.v[u][2 * e + 1], sc);
         }
         if (odd) atomicOr(&odd_in[j & 3], odd);
     };
@@ -167,16 +171,19 @@ cache_prompt_kernel(CacheAttnArgs a)
     float m = M_NONE, l = 0.f;
 
     if (threadIdx.x < 4) odd_in[threadIdx.x] = 0;
+    Pages pages;
+    Codes codes;
     if (begin < end) {
-        load_pages(begin);
-        load(begin);
-        if (begin + 1 < end) load_pages(begin + 1);
-    }
-    __syncthreads();
-    if (begin < end) {
-        stage(begin, begin & 1);
-        if (begin + 1 < end) load(begin + 1);
-        if (begin + 2 < end) load_pages(begin + 2);
+        // the first two steps' codes are on their way together
+        Pages pages1;
+        Codes codes0;
+        load_pages(begin, pages);
+        load_pages(min(begin + 1, end - 1), pages1);
+        load(begin, pages, codes0);
+        load(min(begin + 1, end - 1), pages1, codes);
+        load_pages(min(begin + 2, end - 1), pages);
+        __syncthreads();
+        stage(begin, begin & 1, codes0);
     }
     __syncthreads();
     // S rows of lane half `half`: register 4 q + i is row 8 q + 4 half + i of the 32, and holds position 16 (q / 2) + 8 half + 4 (q & 1) + i
@@ -191,9 +198,9 @@ cache_prompt_kernel(CacheAttnArgs a)
     for (int j = begin; j < end; ++j) {
         const int buf = j & 1, pos = range.position(j);
         if (j + 1 < end) {
-            stage(j + 1, buf ^ 1);
-            if (j + 2 < end) load(j + 2);
-            if (j + 3 < end) load_pages(j + 3);
+            stage(j + 1, buf ^ 1, codes);
+            if (j + 2 < end) load(j + 2, pages, codes);
+            if (j + 3 < end) load_pages(j + 3, pages);
         }
         if (threadIdx.x == 0) odd_in[(j + 2) & 3] = 0;            // last read two steps ago, next written in the next one
         const int odd = odd_in[j & 3];
@@ -334,26 +341,80 @@ cache_prompt_kernel(CacheAttnArgs a)
 }
 
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
-static int64_t prompt_items(int B, int Hkv, int G, int N) { return (int64_t)B * Hkv * (((int64_t)N * G + PROMPT_ROWS - 1) / PROMPT_ROWS); }
 
-// Pieces per item: as many workgroups as the chip holds (two per CU), where there are fewer items.
-int prompt_parts(int B, int Hkv, int G, int N)
+// Joins the pieces of items in several: the workgroups of an item (gridDim.y of them) share its rows, a thread has 4 channels of a row at a time.
+template <int D>
+__global__ void __launch_bounds__(512)
+cache_parts_join_kernel(CacheAttnArgs a)
 {
-    return (int)std::max<int64_t>(1, std::min<int64_t>(32, 2 * cache_cus() / prompt_items(B, Hkv, G, N)));
+    constexpr int CH = D / 4, ROWS = PROMPT_ROWS, U = 8;
+    unsigned item = blockIdx.x;
+    const int tile = item % (unsigned)a.row_tiles;
+    const int h = item / (unsigned)a.row_tiles % (unsigned)a.c.Hkv, b = item / (unsigned)a.row_tiles / (unsigned)a.c.Hkv;
+    const SeqInfo sq = seq_of(a, b);
+    const int rows = (int)min((int64_t)sq.n * a.G - (int64_t)tile * ROWS, (int64_t)ROWS);
+    if (rows <= 0) return;
+    const int parts = parts_of(range_of<ROWS, false>(a, sq, tile).steps, a.parts);
+    if (parts == 1) return;
+    const float* first = a.pieces + (int64_t)item * a.parts * (ROWS * (D + 2));
+    for (int at = blockIdx.y * 512 + threadIdx.x; at < rows * CH; at += gridDim.y * 512) {
+        const int rr = at / CH, ch = at % CH;
+        v4f o = {0.f, 0.f, 0.f, 0.f};
+        float m = M_NONE, l = 0.f;
+        for (int w = 0; w < parts; w += U) {
+            float m2[U], l2[U];
+            v4f x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                m2[u] = M_NONE;
+                l2[u] = 0.f;
+                x[u] = v4f{0.f, 0.f, 0.f, 0.f};
+                if (w + u < parts) {                                      // the same for all threads
+                    const float* p = first + (int64_t)(w + u) * (ROWS * (D + 2));
+                    m2[u] = p[ROWS * D + rr];
+                    l2[u] = p[ROWS * D + ROWS + rr];
+                    x[u] = *(const v4f*)(p + rr * D + ch * 4);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (w + u >= parts) break;
+                const float up = fmaxf(m, m2[u]);
+                const float f1 = __builtin_amdgcn_exp2f((m - up) * a.scale), f2 = __builtin_amdgcn_exp2f((m2[u] - up) * a.scale);
+                m = up;
+                l = l * f1 + l2[u] * f2;
+                o = o * f1 + x[u] * f2;
+            }
+        }
+        const int r = tile * ROWS + rr, i = r / a.G;
+        char* op = a.out.data + b * a.out.stride_batch + (h * a.G + r - i * a.G) * a.out.stride_head + i * a.out.stride_token;
+        const v4f x = o * (l == 0.f ? 0.f : 1.f / l);
+        *(v2i*)(op + ch * 8) = v2i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    }
 }
 
-size_t cache_prompt_workspace(int B, int Hkv, int G, int N, int D)
+static int64_t prompt_items(int B, int Hkv, int G, int N) { return (int64_t)B * Hkv * (((int64_t)N * G + PROMPT_ROWS - 1) / PROMPT_ROWS); }
+
+// Pieces per item: as many workgroups as the chip holds (two per CU), where there are fewer items, of at least two of the steps that an item
+// can reach.  (16 items of 128 steps: 33.0 us in the other kernel's shares, 28.6 in 32 pieces; 128 items of 125 steps 188 us whole, 103 in 4.)
+static int prompt_parts(int B, int Hkv, int G, int N, int64_t reach)
 {
-    const int parts = prompt_parts(B, Hkv, G, N);
+    const int64_t most = std::min<int64_t>(32, reach / STEP / 2);
+    return (int)std::max<int64_t>(1, std::min(most, 2 * cache_cus() / prompt_items(B, Hkv, G, N)));
+}
+
+size_t cache_prompt_workspace(int B, int Hkv, int G, int N, int D, int64_t reach)
+{
+    const int parts = prompt_parts(B, Hkv, G, N, reach);
     return parts > 1 ? (size_t)(prompt_items(B, Hkv, G, N) * parts * PROMPT_ROWS * (D + 2) * 4) : 0;
 }
 
-int launch_cache_prompt(CacheAttnArgs a, void* workspace, hipStream_t stream)
+int launch_cache_prompt(CacheAttnArgs a, int64_t reach, void* workspace, hipStream_t stream)
 {
     constexpr int NW = PROMPT_WAVES;
     const int64_t items = prompt_items(a.s.B, a.c.Hkv, a.G, a.s.N);
     a.row_tiles = (int)(items / a.s.B / a.c.Hkv);
-    a.parts = prompt_parts(a.s.B, a.c.Hkv, a.G, a.s.N);
+    a.parts = prompt_parts(a.s.B, a.c.Hkv, a.G, a.s.N, reach);
     a.pieces = (float*)workspace;
     if (items * a.parts * 64 * NW > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
     const dim3 grid((unsigned)(items * a.parts)), block(64 * NW);
@@ -361,7 +422,7 @@ int launch_cache_prompt(CacheAttnArgs a, void* workspace, hipStream_t stream)
         int rc = a.c.page_shift >= 6 ? launch(cache_prompt_kernel<D, E5M2 != 0, NW, true>, grid, block, stream, a)
                                      : launch(cache_prompt_kernel<D, E5M2 != 0, NW, false>, grid, block, stream, a);
         if (rc == DMA_OK_ && a.parts > 1)
-            rc = launch(cache_attn_join_kernel<D, PROMPT_ROWS, true>, dim3((unsigned)items, PROMPT_ROWS / 4), dim3(1024), stream, a);
+            rc = launch(cache_parts_join_kernel<D>, dim3((unsigned)items, (unsigned)std::min(a.parts, PROMPT_ROWS * D / 4 / 512)), dim3(512), stream, a);
         return rc;
     };
     if (a.c.D == 128) return a.c.e5m2 ? go(IC<128>{}, IC<1>{}) : go(IC<128>{}, IC<0>{});
