@@ -365,6 +365,8 @@ def dma_cache_attn(q: torch.Tensor, cache: KVCache, start: torch.Tensor, n_token
     if out is None:
         out = torch.zeros(shape, dtype=_BF16, device=cache.device)
     ro = _rows(out, "out", shape, index)
+    if not (0 <= window < 1 << 31 and 0 <= sink_tokens < 1 << 31):
+        raise ValueError("window and sink_tokens must be in [0, 2^31)")
     L = load()
     if workspace is None:
         pw, nw = None, L.dma_cache_attn_workspace_bytes(cache._ref, B, Hq, N, window, sink_tokens)

@@ -33,6 +33,8 @@ cache_attn_kernel(CacheAttnArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
     __shared__ __attribute__((aligned(16))) float obuf[W][ROWS][LD];
     __shared__ float ml[W][2][ROWS];
+    // with 32 rows, the queries' operands, of which each wave loads some: in registers they would be spilled, and a reload waits for the codes in flight
+    __shared__ __attribute__((aligned(16))) v8bf qs[MT > 1 ? MT : 1][MT > 1 ? 2 * KJ : 1][MT > 1 ? 64 : 1];
     const CacheView& c = a.c;
     const int page_mask = (1 << c.page_shift) - 1;
 
@@ -136,18 +138,21 @@ cache_attn_kernel(CacheAttnArgs a)
     // ---- item after item.  The codes of an item's first steps are requested before the sums of the one before it are joined.
     StepRange range = {0, 0, 0};
     int weight = 1, until = 0, rows = 0, all_hi = 0, all_lo = 0, last = 0, j = 0;
-    v8bf qf[MT][2 * KJ];
+    v8bf qf[MT == 1 ? 2 * KJ : (MT * 2 * KJ + W - 1) / W];
     int vis_lo[MT], vis_hi[MT];              // what the row of this lane's column sees: these positions and those below sinks
     const int* table = nullptr;
     v4i kr[4][KJ], vr[DT];
     uint8_t k_scale = 0, v_scale = 0;
     int v_page = -1, pk = -1, pv = -1;       // pages of the step after the next
-    // Pages of a step: of the 16 positions whose keys this lane loads, and of those whose values it loads.
+    // Pages of a step: of the 16 positions whose keys this lane loads, and of those whose values it loads.  Requested a step ahead, and
+    // looked at (behind the table: no page) only where they are used: looking at once would wait for the codes too.
     auto page_of = [&](int jj, int g) -> int {
-        const int pi = (range.position(jj) + (UNI ? 0 : 16 * g)) >> c.page_shift;
-        const int at = min(pi, c.max_pages - 1);
-        const int page = UNI ? scalar_at(table, __builtin_amdgcn_readfirstlane(at)) : table[at];
-        return pi < c.max_pages ? page : -1;
+        const int at = min((range.position(jj) + (UNI ? 0 : 16 * g)) >> c.page_shift, c.max_pages - 1);
+        return UNI ? scalar_at(table, __builtin_amdgcn_readfirstlane(at)) : table[at];
+    };
+    auto there = [&](int page, int jj, int g) -> int {
+        if constexpr (!UNI) asm volatile("" : "+v"(page));
+        return (range.position(jj) + (UNI ? 0 : 16 * g)) >> c.page_shift < c.max_pages ? page : -1;
     };
     auto slab_of = [&](int page) -> int64_t {
         if constexpr (UNI) page = __builtin_amdgcn_readfirstlane(page);
@@ -199,9 +204,9 @@ cache_attn_kernel(CacheAttnArgs a)
                 const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = token_of<ONE>(a, r);
                 const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + r - i * a.G) * a.q.stride_head + i * a.q.stride_token;
 #pragma unroll
-                for (int jj = 0; jj < KJ; ++jj)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) qf[mt][2 * jj + e] = *(const v8bf*)(qp + (jj * 64 + grp * 16 + e * 8) * 2);
+                for (int ks = 0; ks < 2 * KJ; ++ks)
+                    if (MT == 1) qf[ks] = *(const v8bf*)(qp + ((ks >> 1) * 64 + grp * 16 + (ks & 1) * 8) * 2);
+                    else if ((mt * 2 * KJ + ks) % W == wave) qf[(mt * 2 * KJ + ks) / W] = *(const v8bf*)(qp + ((ks >> 1) * 64 + grp * 16 + (ks & 1) * 8) * 2);
                 vis_hi[mt] = (int)min(from + i, (int64_t)POS_MAX);
                 vis_lo[mt] = a.window ? (int)min(max(from + i - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
             }
@@ -210,10 +215,11 @@ cache_attn_kernel(CacheAttnArgs a)
             all_lo = a.window ? (int)min(max(from + token_of<ONE>(a, tile * ROWS + rows - 1) - a.window + 1, (int64_t)0), (int64_t)POS_MAX) : 0;
             __builtin_amdgcn_sched_barrier(0);
             if (j < last) {
-                load_k(j, pk, true);
-                load_v(j, pv, true);
+                const int page_v = there(pv, j, grp);
+                load_k(j, there(pk, j, col >> 2), true);
                 pk = page_of(min(j + W, last - 1), col >> 2);
                 pv = UNI ? pk : page_of(min(j + W, last - 1), grp);
+                load_v(j, page_v, true);
             }
         }
 
@@ -256,7 +262,13 @@ cache_attn_kernel(CacheAttnArgs a)
                 }
             }
             if (!more) return;
-            __syncthreads();                                      // before the next item's sums
+            if constexpr (MT == 1) __syncthreads();               // before the next item's sums
+        }
+        if constexpr (MT > 1) {
+#pragma unroll
+            for (int f = 0; f < MT * 2 * KJ; ++f)
+                if (f % W == wave) qs[f / (2 * KJ)][f % (2 * KJ)][lane] = qf[f / W];
+            __syncthreads();
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -266,14 +278,14 @@ cache_attn_kernel(CacheAttnArgs a)
             l[mt] = 0.f;
         }
         // the queries, requested first, have arrived before the loop: no wait for them inside it, which would be one for the codes
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        if constexpr (MT == 1) {
 #pragma unroll
             for (int ks = 0; ks < 2 * KJ; ++ks) {
-                v4i w = __builtin_bit_cast(v4i, qf[mt][ks]);
+                v4i w = __builtin_bit_cast(v4i, qf[ks]);
                 asm volatile("" : "+v"(w));
-                qf[mt][ks] = __builtin_bit_cast(v8bf, w);
+                qf[ks] = __builtin_bit_cast(v8bf, w);
             }
+        }
         for (; j < last; j += W) {
             // the codes of the next step are requested without a branch (what the compiler cannot count it waits for in full):
             // behind the last step, one address for all lanes
@@ -288,6 +300,13 @@ cache_attn_kernel(CacheAttnArgs a)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) s[mt][t] = v4f{0.f, 0.f, 0.f, 0.f};
             const float ksc = __int_as_float(k_scale << 23);
+            v8bf qk[MT][2 * KJ];
+            int mine = lane;
+            if constexpr (MT > 1) asm volatile("" : "+v"(mine));  // (so that they are not read once, before the loop, after all)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int ks = 0; ks < 2 * KJ; ++ks) qk[mt][ks] = MT == 1 ? qf[ks] : qs[MT > 1 ? mt : 0][MT > 1 ? ks : 0][MT > 1 ? mine : 0];
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -296,11 +315,11 @@ cache_attn_kernel(CacheAttnArgs a)
                     for (int e = 0; e < 2; ++e) {
                         const v8bf k = decode8<E5M2>(kr[t][jj][2 * e], kr[t][jj][2 * e + 1], ksc);
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) s[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[mt][2 * jj + e], s[mt][t], 0, 0, 0);
+                        for (int mt = 0; mt < MT; ++mt) s[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qk[mt][2 * jj + e], s[mt][t], 0, 0, 0);
                     }
             // ---- the next step's keys, the pages of the one after it
-            const int page_v = pv;
-            load_k(next, pk, more);
+            const int page_v = there(pv, next, grp);
+            load_k(next, there(pk, next, col >> 2), more);
             pk = page_of(min(j + 2 * W, last - 1), col >> 2);
             pv = UNI ? pk : page_of(min(j + 2 * W, last - 1), grp);
             // ---- what is not seen
@@ -520,7 +539,8 @@ static int mt_of(int G, int N) { return (int64_t)G * N <= 16 ? 1 : 2; }
 // 32 of 0.4k-4k (256 items) 37.1, 41.7; 64 of 16k (512 items) 358, 377; 32 rows: 16 of 4k x 16 tokens (256 items) 52.8, 49.1; 16 of 2k x 17 tokens, 32
 // kv heads (512 items) 70.5, 77.4.
 static int waves_of(int mt, int64_t items) { return items <= (mt == 1 ? cache_cus() / 2 : cache_cus()) ? 8 : 4; }
-static int64_t grid_of(int waves) { return (int64_t)cache_cus() * 8 / waves; }
+// (A multiple of 8, for the order over the XCDs.)
+static int64_t grid_of(int waves) { return ((int64_t)cache_cus() * 8 / waves + 7) / 8 * 8; }
 
 // Whether the kernel for many rows serves the call: where the other one would need more than two tiles of 32 rows (us with either, 16
 // sequences of 4k: 64 rows 52.9 and 56.7, 96 rows 86.7 and 63.3; D = 64, 64 sequences: 64 rows 103 and 98, 124 rows 191 and 115), and at D = 128 with

@@ -450,6 +450,52 @@ def test_graph_follows_start():
         assert torch.equal(dma.dma_kv_read(pair.gpu, start, 1)[0], dma.dma_kv_read(other.gpu, start, 1)[0])
 
 
+@pytest.mark.parametrize("N,Hq", [(1, 4), (6, 8), (40, 4)])
+def test_two_graphs_with_one_workspace(N, Hq):
+    """Calls whose pieces are joined by a second kernel, captured in two graphs that are given the same workspace, replayed in turn and
+    with other lengths, eager calls with their own workspace in between."""
+    rng = np.random.default_rng(N)
+    B, Hkv, D, P = 3, 2, 128, 64
+    pair = filled(rng, [3000, 1500, 100], Hkv, P, D, "e4m3")
+    start = i32([2900, 1400, 50])
+    need = dma.dma_cache_attn_workspace_bytes(pair.gpu, Hq, N)
+    assert need > 0
+    ws = torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
+    qs = [bf16(rng, B, Hq, N, D).cuda() for _ in range(2)]
+    outs, graphs, side = [torch.zeros_like(q) for q in qs], [], torch.cuda.Stream()
+    for q, o in zip(qs, outs):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            dma.dma_cache_attn(q, pair.gpu, start, out=o, workspace=ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            dma.dma_cache_attn(q, pair.gpu, start, out=o, workspace=ws)
+    for lens in ([2900, 1400, 50], [10, 1400, 60], [2960, 0, 0], [700, 701, 55]):
+        start.copy_(i32(lens))
+        for _ in range(2):
+            for g, q, o in zip(graphs, qs, outs):
+                o.zero_()
+                torch.cuda.synchronize()
+                g.replay()
+                eager = dma.dma_cache_attn(q, pair.gpu, start)
+                torch.cuda.synchronize()
+                assert torch.equal(o, eager), lens
+    pair.attn(qs[0], lens)
+
+
+def test_no_page_at_all():
+    """A cache without pages under a table of thousands: nothing is read, rows are zeros."""
+    empty = lambda *s: torch.empty(s, dtype=torch.uint8, device="cuda")
+    cache = dma.KVCache(empty(0, 2, 64, 128), empty(0, 2, 128, 64), empty(0, 2), empty(0, 2), torch.full((3, 5000), 7, dtype=torch.int32, device="cuda"))
+    for N in (1, 8, 70):
+        x = torch.ones((3, 4, N, 128), dtype=torch.bfloat16, device="cuda")
+        out = torch.ones_like(x)
+        assert not dma.dma_cache_attn(x, cache, i32([300000, 5, 0]), out=out).any()
+        dma.dma_kv_write(cache, x[:, :2], x[:, 2:], i32([300000, 5, 0]))
+        assert (dma.dma_kv_read(cache, i32([300000, 5, 0]), out=(out[:, :2], x[:, :2]))[1] == 1).all()
+
+
 def test_equal_calls_give_equal_bits_on_any_stream():
     rng = np.random.default_rng(9)
     pair = filled(rng, [1900, 3, 700], 2, 32, 128, "e4m3")

@@ -156,6 +156,7 @@ def test_binding_checks_shapes(handle, monkeypatch):
         dma.dma_kv_read(handle, start, 5, out=(kv, kv))
     for args, kw in (((on_gpu(3, 8, 64),), {}), ((on_gpu(3, 8, 4, 128),), {}), ((q,), dict(out=on_gpu(3, 8, 5, 64))), ((q,), dict(out=on_gpu(3, 8, 4, 64, dtype=torch.float32))),
                      ((q,), dict(out=on_gpu(3, 8, 4, 128)[..., ::2])), ((q,), dict(out=q, workspace=torch.zeros(9, dtype=torch.uint8))),
+                     ((q,), dict(out=q, window=-1)), ((q,), dict(out=q, window=1 << 31)), ((q,), dict(out=q, sink_tokens=(1 << 32) + 1)),
                      ((torch.zeros((3, 8, 4, 64), dtype=torch.bfloat16),), {})):
         with pytest.raises(ValueError):
             dma.dma_cache_attn(*args, handle, start, **kw)
