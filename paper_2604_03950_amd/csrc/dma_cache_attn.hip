@@ -536,19 +536,20 @@ static int mt_of(int G, int N) { return (int64_t)G * N <= 16 ? 1 : 2; }
 // Waves of a workgroup where the steps are cut in shares; the chip holds 8 / waves of them per CU.  Eight where items are few: half the starts
 // and pieces for the same bytes.  Four otherwise: the waves of a workgroup end an item together, so eight leave more of a CU idle at its
 // end.  us with four and with eight, 16 rows: one sequence of 8k (8 items) 15.3, 13.2; of 128k 56.0, 53.8; 16 of 4k (128 items) 32.0, 31.6;
-// 32 of 0.4k-4k (256 items) 37.1, 41.7; 64 of 16k (512 items) 358, 377; 32 rows: 16 of 4k x 16 tokens (256 items) 52.8, 49.1; 16 of 2k x 17 tokens, 32
-// kv heads (512 items) 70.5, 77.4.
+// 32 of 0.4k-4k (256 items) 37.1, 41.7; 64 of 16k (512 items) 358, 377; 32 rows: 16 of 4k x 16 tokens (256 items) 49.2, 44.0;
+// 32 of 2k x 16 tokens (512 items) 52.0, 64.2.
 static int waves_of(int mt, int64_t items) { return items <= (mt == 1 ? cache_cus() / 2 : cache_cus()) ? 8 : 4; }
 // (A multiple of 8, for the order over the XCDs.)
 static int64_t grid_of(int waves) { return ((int64_t)cache_cus() * 8 / waves + 7) / 8 * 8; }
 
-// Whether the kernel for many rows serves the call: where the other one would need more than two tiles of 32 rows (us with either, 16
-// sequences of 4k: 64 rows 52.9 and 56.7, 96 rows 86.7 and 63.3; D = 64, 64 sequences: 64 rows 103 and 98, 124 rows 191 and 115), and at D = 128 with
-// 17 rows and more where every sequence and kv head finds a place on the chip (16 sequences of 2k, 32 kv heads: 17 rows 70.5 and 59.6, 64 rows 119 and 77).
-static bool many_rows(int B, int Hkv, int G, int N, int D)
+// Whether the kernel for many rows serves the call: where the other one would need more than two tiles of 32 rows, and with two of them
+// where sequences and kv heads alone give every CU an item of 128 rows.  us with the kernel for few and the one for many: 32 rows,
+// 64 sequences of 0.4k-4k 92.8, 100; 64 rows: 16 of 4k (128 pairs) 44.0, 49.6; 32 of 2k (256) 52.2, 58.7; 64 of 0.4k-4k (512) 130, 114;
+// 16 of 2k, 32 kv heads (512) 109, 77; D = 64, 64 of 2k (512) 65.1, 53.4; 80 rows: 16 of 4k 81.5, 53.0; one of 32k 42.4, 39.0.
+static bool many_rows(int B, int Hkv, int G, int N)
 {
     const int64_t rows = (int64_t)N * G;
-    return rows > 64 || (rows > 16 && D == 128 && (int64_t)B * Hkv >= 2 * cache_cus());
+    return rows > 64 || (rows > 32 && (int64_t)B * Hkv > cache_cus());
 }
 
 // The most positions that a row tile can visit.
@@ -564,7 +565,7 @@ constexpr int64_t SHORT_REACH = 20 * STEP;
 size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window, int sinks)
 {
     const int G = Hq / c.Hkv;
-    if (many_rows(B, c.Hkv, G, N, c.D)) return cache_prompt_workspace(B, c.Hkv, G, N, c.D, reach_of(c, 128, G, window, sinks));
+    if (many_rows(B, c.Hkv, G, N)) return cache_prompt_workspace(B, c.Hkv, G, N, c.D, reach_of(c, 128, G, window, sinks));
     const int mt = mt_of(G, N), rows = 16 * mt;
     if (reach_of(c, rows, G, window, sinks) <= SHORT_REACH) return 0;
     const int64_t tiles = ((int64_t)N * G + rows - 1) / rows, items = (int64_t)B * c.Hkv * tiles;
@@ -611,7 +612,7 @@ int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const 
     a.sinks = window ? sinks : 0;
     a.capacity = c.num_pages ? c.max_pages << c.page_shift : 0;
     a.scale = (float)(1.4426950408889634074 / sqrt((double)c.D));
-    if (many_rows(s.B, c.Hkv, a.G, s.N, c.D)) return launch_cache_prompt(a, reach_of(c, 128, a.G, window, a.sinks), workspace, stream);
+    if (many_rows(s.B, c.Hkv, a.G, s.N)) return launch_cache_prompt(a, reach_of(c, 128, a.G, window, a.sinks), workspace, stream);
     const int mt = mt_of(a.G, s.N);
     auto pick = [&](auto D, auto F) { return mt == 1 ? launch_few<D, F != 0, 1>(a, workspace, stream) : launch_few<D, F != 0, 2>(a, workspace, stream); };
     if (c.D == 128) return c.e5m2 ? pick(IC<128>{}, IC<1>{}) : pick(IC<128>{}, IC<0>{});

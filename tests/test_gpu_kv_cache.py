@@ -240,6 +240,18 @@ def test_many_rows(fmt, D, P, G, N, window, sinks):
     assert (got.float().cpu().numpy()[~rows] == 7).all()
 
 
+@pytest.mark.parametrize("fmt,D,N,G", [("e4m3", 128, 16, 2), ("e4m3", 128, 33, 1), ("e5m2", 64, 16, 4), ("e4m3", 64, 5, 13)])
+@pytest.mark.parametrize("B", [9, 66])
+def test_between_few_and_many_rows(B, fmt, D, N, G):
+    """32, 33, 64 and 65 rows per kv head, for few and for many sequences."""
+    rng = np.random.default_rng(N * G + B)
+    n = rng.integers(1, N + 1, B)
+    n[:2] = N
+    start = rng.integers(0, 150, B)
+    pair = filled(rng, list(start + n), 4, 32, D, fmt)
+    pair.attn(bf16(rng, B, 4 * G, N, D), start, n)
+
+
 @pytest.mark.parametrize("N,G,D,window", [(1, 4, 128, 0), (3, 4, 64, 0), (7, 8, 128, 0), (1, 16, 64, 1500), (9, 2, 128, 2000)])
 def test_long_and_short_sequences_together(N, G, D, window):
     """More sequences than a workgroup has threads, a few long ones among them: shares that hold many sequences, sequences that
