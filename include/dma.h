@@ -4,17 +4,20 @@
  *
  * Conventions for every call
  *   - Every data pointer is a DEVICE pointer owned by the caller (e.g. the storage of a PyTorch
- *     tensor); the library allocates nothing and writes only to the output buffers named below.  The only
- *     state it keeps between calls is read-only once filled: the compute-unit count per device and the
- *     number of resident workgroups per kernel instance, both queried from the runtime on first use.
+ *     tensor); the library allocates nothing and writes only to the output buffers named below (and to the
+ *     workspace, where a call takes one).  The only state it keeps between calls is read-only once filled: the
+ *     compute-unit count per device and the number of resident workgroups per kernel instance, both queried from
+ *     the runtime on first use.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Calls enqueue their
  *     kernels on it and return without waiting.  They issue nothing but kernel launches (no
  *     allocation, copy, memset or synchronisation), so a stream under HIP graph capture records
  *     them and the graph can be replayed.
  *   - Return value: DMA_OK (0) or a negative error code.  On error nothing has been enqueued.
  *     No C++ exception crosses the boundary.  dma_error_string() maps a code to a static string.
- *   - bf16 tensors are dense and row-major with the head dimension D innermost.
- *   - Inputs are assumed finite; NaN/Inf give unspecified results (never a fault).
+ *   - bf16 tensors are row-major with the head dimension D innermost, and dense; of a tensor passed as dma_rows only
+ *     the rows of D elements are.
+ *   - Inputs are assumed finite; NaN/Inf give unspecified results (never a fault).  What the calls on a key / value cache do
+ *     with those among keys and values is said there.
  */
 #ifndef DMA_H_
 #define DMA_H_
@@ -250,8 +253,10 @@ int dma_kv_read(const dma_kv_cache* cache, const dma_rows* k_out, const dma_rows
  *   The query at position p sees the keys at positions t <= p and, if window > 0, of these only t > p - window and
  *   t < sink_tokens (the first tokens of the sequence stay visible).  window = 0: no window, sink_tokens has no effect.
  *   A query that sees no key (none of the positions it could see has a page) gives zeros.
- *   Positions that are not seen may hold anything, NaN codes among it.
- * Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 for the second product, as in dma_attn_fwd.
+ *   Positions that are not seen may hold anything, NaN codes among it.  A NaN among the keys that a query sees makes its
+ *   row NaN, one among the values that channel of it.
+ * Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 for the second product, as in dma_attn_fwd,
+ * and the sum that divides them adds the rounded ones.
  * Equal calls give equal bits; the order of the sums over the keys follows from the sizes and the values of start and n_tokens.
  *   workspace  device, 16-byte aligned, at least dma_cache_attn_workspace_bytes(...) bytes (NULL if that is 0); not
  *              initialised by the caller, without meaning after the call.  Calls that may run at the same time need one each.

@@ -28,11 +28,11 @@ HIPCC_FLAGS = [
 
 
 def source_digest() -> str:
-    """SHA-256 over the kernel sources and the public header (file names and contents, sorted by name): what a profile
-    summary records so that a figure measured on one version of the kernels is not quoted for another."""
+    """SHA-256 over the sources of the forward and the quantizers and the public header (file names and contents, sorted by
+    name): what a profile summary records so that a figure measured on one version of the kernels is not quoted for another."""
     import hashlib
     h = hashlib.sha256()
-    names = sorted(n for n in os.listdir(CSRC) if n.endswith((".hip", ".hpp")))
+    names = sorted(n for n in os.listdir(CSRC) if n.endswith((".hip", ".hpp")) and not n.startswith("dma_cache"))
     for path in [os.path.join(CSRC, n) for n in names] + [os.path.join(HERE, "..", "include", "dma.h")]:
         h.update(os.path.basename(path).encode() + b"\0")
         with open(path, "rb") as f:

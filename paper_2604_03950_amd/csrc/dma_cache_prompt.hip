@@ -3,8 +3,12 @@
 // A workgroup of NW waves takes 32 * NW rows (query tokens times the query heads of a kv head, token by token); every wave has 32 of
 // them, and all walk the same steps of 64 positions.  The codes of a step are decoded to bf16 once per workgroup, into LDS (exact: the
 // page's scale is applied), one step ahead of their use; one barrier per step.  As in the kernel for few rows, S^T = K Q^T takes its key
-// rows in an order that leaves every probability in the lane that needs it for O^T = V^T P^T, and the softmax's maximum is raised only when
-// a score exceeds it by 8 units of base 2.
+// rows in an order that leaves every probability in the lane that needs it for O^T = V^T P^T, and the softmax's maximum is raised only
+// where the sum of a lane's 32 probabilities exceeds 1024.
+//
+// Measured, 32 query and 8 kv heads, D = 128: 2048 tokens behind 14k 545 to 590 us = 0.87 to 0.95 PFLOP/s, 4096 behind 28k 0.98 (a bf16 matrix product
+// of 8192^3 runs at 1.15 here); 512 behind 7.5k 91 us = 0.73; 8192 under a window of 1024 180 to 205 us, 0.63 to 0.72 of the visible pairs' flops.  Two
+// workgroups of four waves per CU: while one waits at the barrier the other's products run; matrix and vector time of a SIMD add up otherwise.
 #include "dma_cache_device.hpp"
 #include <algorithm>
 #include <math.h>
@@ -79,17 +83,24 @@ cache_prompt_kernel(CacheAttnArgs a)
         const int page = UNI ? scalar_at(table, at) : table[at];
         return pi < c.max_pages ? page : -1;
     };
+    // Which 16 codes a thread has: 8 lanes write to LDS in one turn, and would find half of its banks with 8 chunks of a key (every second
+    // one of a row) or 4 of two channels (whose rows are shifted alike): 4 of a key and 4 of the next, 4 of a channel and 4 of the next but one
+    // (4096 tokens behind 28k 2062 us, 2086 without).
+    auto next_but_one = [](int row) { return (row & ~3) | (row & 1) << 1 | (row >> 1 & 1); };
+    auto key_of = [&](int ch) { return D == 128 ? (ch >> 2 & 1) | ch >> 4 << 1 : next_but_one(ch / 4); };
+    auto part_of = [](int ch) { return D == 128 ? (ch & 3) | (ch >> 1 & 4) : ch & 3; };
+    auto channel_of = [&](int ch) { return next_but_one(ch / 4); };
     auto load_pages = [&](int j, Pages& pg) {                     // one step before load(), two before stage()
         const int pos = range.position(j);
         if constexpr (UNI) pg.k[0] = page_at(pos);
         else {
 #pragma unroll
-            for (int u = 0; u < KCH; ++u) pg.k[u] = page_at(pos + (threadIdx.x + u * T) / (D / 16));
+            for (int u = 0; u < KCH; ++u) pg.k[u] = page_at(pos + key_of(threadIdx.x + u * T));
 #pragma unroll
             for (int u = 0; u < VCH; ++u) pg.v[u] = page_at(pos + (threadIdx.x & 3) * 16);
         }
     };
-    const unsigned kofs = threadIdx.x * 16, vofs = (threadIdx.x / 4 << c.page_shift) + (threadIdx.x & 3) * 16;
+    const unsigned kofs = key_of(threadIdx.x) * D + part_of(threadIdx.x) * 16, vofs = (channel_of(threadIdx.x) << c.page_shift) + (threadIdx.x & 3) * 16;
     auto load = [&](int j, const Pages& pg, Codes& cd) {
         const int pos = range.position(j);
         if constexpr (UNI) {
@@ -106,9 +117,9 @@ cache_prompt_kernel(CacheAttnArgs a)
         } else {
 #pragma unroll
             for (int u = 0; u < KCH; ++u) {
-                const int ch = threadIdx.x + u * T, p = pos + ch / (D / 16);
+                const int ch = threadIdx.x + u * T, p = pos + key_of(ch);
                 const int64_t slab = (int64_t)((unsigned)pg.k[u] < c.page_limit ? pg.k[u] : 0) * c.Hkv + h;
-                cd.k[u] = *(const v4i*)(c.k_codes + (((slab << c.page_shift) + (p & page_mask)) * D + ch % (D / 16) * 16));
+                cd.k[u] = *(const v4i*)(c.k_codes + (((slab << c.page_shift) + (p & page_mask)) * D + part_of(ch) * 16));
                 cd.ksc[u] = c.k_scales[slab];
             }
 #pragma unroll
@@ -116,7 +127,7 @@ cache_prompt_kernel(CacheAttnArgs a)
                 const int ch = threadIdx.x + u * T, p = pos + (ch & 3) * 16;
                 cd.there[u] = (unsigned)pg.v[u] < c.page_limit;
                 const int64_t slab = (int64_t)(cd.there[u] ? pg.v[u] : 0) * c.Hkv + h;
-                cd.v[u] = *(const v4i*)(c.v_codes + (((slab * D + ch / 4) << c.page_shift) + (p & page_mask)));
+                cd.v[u] = *(const v4i*)(c.v_codes + (((slab * D + channel_of(ch)) << c.page_shift) + (p & page_mask)));
                 cd.vsc[u] = c.v_scales[slab];
             }
         }
@@ -128,7 +139,7 @@ cache_prompt_kernel(CacheAttnArgs a)
         const int pos = range.position(j);
 #pragma unroll
         for (int u = 0; u < KCH; ++u) {
-            const int ch = threadIdx.x + u * T, key = ch / (D / 16), d16 = ch % (D / 16);
+            const int ch = threadIdx.x + u * T, key = key_of(ch), d16 = part_of(ch);
             const int shift = shift_of((key & 3) | (key >> 1 & 4) | (key << 1 & 8), KROW);
             const float sc = __int_as_float(cd.ksc[UNI ? 0 : u] << 23);
 #pragma unroll
@@ -141,7 +152,7 @@ cache_prompt_kernel(CacheAttnArgs a)
         int odd = 0;
 #pragma unroll
         for (int u = 0; u < VCH; ++u) {
-            const int ch = threadIdx.x + u * T, d = ch / 4;
+            const int ch = threadIdx.x + u * T, d = channel_of(ch);
             const float sc = __int_as_float(cd.vsc[UNI ? 0 : u] << 23);
             const bool there = cd.there[UNI ? 0 : u];
             if (!there) odd |= 1 << (ch & 3);
