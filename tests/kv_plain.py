@@ -111,7 +111,8 @@ class Cache:
         """q: float64 [B, Hq, N, D] -> (out, bound): out NaN in rows that do not exist, and how far a bf16 result may be off.
 
         The bound counts: the result's rounding to bf16, half a step of 2^-8 of itself; the probabilities' rounding to bf16, half
-        a step of 2^-8 each, of the probability-weighted mean of |v|; the binary32 scores, whose sums of D products are off by at
+        a step |d_t| <= 2^-8 each.  The sum that divides adds the rounded ones, so sum p_t (1 + d_t) v_t / sum p_t (1 + d_t) - o =
+        sum p_t d_t (v_t - o) / sum p_t (1 + d_t), at most 2^-8 (1 + 2^-8) of the probability-weighted mean of |v| plus |o|; the binary32 scores, whose sums of D products are off by at
         most (D + 4) * 2^-24 of the sum of magnitudes (products of bf16 are exact; the factor log2(e) / sqrt(D), the subtraction of the
         maximum and their rounding are the 4), twice, as the row's sum divides; and the binary32 sums over n keys, exp2 and the
         division, at most (n + 32) * 2^-24 of that mean, twice.  Differences between hardware exp2 and the exact one (2 units of
@@ -141,6 +142,6 @@ class Cache:
                     w /= w.sum()
                     out[b, h, i] = w @ vv
                     mean = w @ np.abs(vv)
-                    bound[b, h, i] = (2 ** -8 * np.abs(out[b, h, i]) + mean * (2 ** -8 * (1 + 2 ** -8) + 2 * (D + 4) * 2 ** -24 * mag
+                    bound[b, h, i] = (2 ** -8 * (2 + 2 ** -8) * np.abs(out[b, h, i]) + mean * (2 ** -8 * (1 + 2 ** -8) + 2 * (D + 4) * 2 ** -24 * mag
                                       + 2 * (seen.sum() + 32) * 2 ** -24) + 2.0 ** -130)
         return out, bound
