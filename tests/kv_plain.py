@@ -116,7 +116,9 @@ class Cache:
         most (D + 4) * 2^-24 of the sum of magnitudes (products of bf16 are exact; the factor log2(e) / sqrt(D), the subtraction of the
         maximum and their rounding are the 4), twice, as the row's sum divides; and the binary32 sums over n keys, exp2 and the
         division, at most (n + 32) * 2^-24 of that mean, twice.  Differences between hardware exp2 and the exact one (2 units of
-        2^-23) are within the 32."""
+        2^-23) are within the 32.  Below 2^-126 numbers may become zero: a result, 2^-126; and an exp2, of a probability or of the
+        factor that brings sums of them (each at most 2^11, against a maximum that may lag by as much) to another maximum, where the
+        largest weighs 1 at least: 2^-126 * 2^11 of every |v|."""
         B, Hq, N, D = q.shape
         out, bound = np.full(q.shape, np.nan), np.zeros(q.shape)
         for b in range(B):
@@ -143,5 +145,5 @@ class Cache:
                     out[b, h, i] = w @ vv
                     mean = w @ np.abs(vv)
                     bound[b, h, i] = (2 ** -8 * (2 + 2 ** -8) * np.abs(out[b, h, i]) + mean * (2 ** -8 * (1 + 2 ** -8) + 2 * (D + 4) * 2 ** -24 * mag
-                                      + 2 * (seen.sum() + 32) * 2 ** -24) + 2.0 ** -130)
+                                      + 2 * (seen.sum() + 32) * 2 ** -24) + 2.0 ** -126 + 2.0 ** -115 * np.abs(vv).sum(0))
         return out, bound

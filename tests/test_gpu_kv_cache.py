@@ -422,6 +422,40 @@ def test_prompt_then_tokens():
     pair.same()
 
 
+@pytest.mark.parametrize("fmt,P", [("e4m3", 16), ("e5m2", 64)])
+def test_drafts_taken_back(fmt, P):
+    """Drafted tokens are written and attended to; the next ones stand from the first refused position on, inside the same page or
+    before its border, with larger and smaller elements than those they replace."""
+    rng = np.random.default_rng(P)
+    B, Hkv, G, D, N = 3, 2, 4, 128, 7
+    start = np.array([3, P - 2, 2 * P + 5])
+    table, pages = table_of(rng, [int(s) + 40 for s in start], P)
+    pair = Pair(rng, None, Hkv, P, D, fmt, table, pages)
+    pair.write(bf16(rng, B, Hkv, 2 * P + 5, D), bf16(rng, B, Hkv, 2 * P + 5, D), [0] * B, start)
+    at = start
+    for step, size in enumerate([1.0, 30.0, 0.01, 200.0]):
+        pair.write(bf16(rng, B, Hkv, N, D) * size, bf16(rng, B, Hkv, N, D) * size, at)
+        pair.same()
+        pair.attn(bf16(rng, B, Hkv * G, N, D), at)
+        at = at + np.array([0, 2, 7]) if step % 2 == 0 else at + np.array([4, 1, 3])
+
+
+@pytest.mark.parametrize("N", [1, 5, 40])
+def test_shared_first_pages(N):
+    """Sequences that begin alike hold the same pages at the front of their table; each goes on in pages of its own."""
+    rng = np.random.default_rng(N)
+    B, Hkv, G, D, P = 5, 2, 4, 64, 32
+    own = 3
+    table = np.concatenate([np.tile(np.array([[4, 0, 7]]), (B, 1)), 8 + rng.permutation(B * own).reshape(B, own)], 1).astype(np.int32)
+    pair = Pair(rng, None, Hkv, P, D, "e4m3", table, 8 + B * own)
+    pair.write(bf16(rng, B, Hkv, 3 * P, D), bf16(rng, B, Hkv, 3 * P, D), [0] * B, [3 * P] + [0] * (B - 1))
+    n = np.array([50, 41, 96, 40, 77])
+    pair.write(bf16(rng, B, Hkv, 96, D), bf16(rng, B, Hkv, 96, D), [3 * P] * B, n)
+    pair.same()
+    pair.attn(bf16(rng, B, Hkv * G, N, D), 3 * P + n - N)
+    pair.attn(bf16(rng, B, Hkv * G, N, D), 3 * P + n - N, None, 70, 5)
+
+
 def test_graph_follows_start():
     """One decoding step (write and attention) in a graph, replayed with other tokens and positions, eager work in between."""
     rng = np.random.default_rng(5)
