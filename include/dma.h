@@ -253,7 +253,8 @@ int dma_kv_read(const dma_kv_cache* cache, const dma_rows* k_out, const dma_rows
  *   The query at position p sees the keys at positions t <= p and, if window > 0, of these only t > p - window and
  *   t < sink_tokens (the first tokens of the sequence stay visible).  window = 0: no window, sink_tokens has no effect.
  *   A query that sees no key (none of the positions it could see has a page) gives zeros.
- *   Positions that are not seen may hold anything, NaN codes among it.  A NaN among the keys that a query sees makes its
+ *   Positions that are not seen may hold anything, NaN codes among it, and the scale of a page of which no position is seen may
+ *   be any byte.  A NaN among the keys that a query sees makes its
  *   row NaN, one among the values that channel of it.
  * Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 for the second product, as in dma_attn_fwd,
  * and the sum that divides them adds the rounded ones.

@@ -352,7 +352,9 @@ cache_attn_kernel(CacheAttnArgs a)
                 any |= __builtin_amdgcn_mov_dpp(any, 0x124, 0xF, 0xF, true);
                 any |= __builtin_amdgcn_mov_dpp(any, 0x128, 0xF, 0xF, true);
                 // values that no row sees may be anything, and a NaN among the others must not reach the rows that do not see it
-                // through a probability of zero: zeros instead, and NaN in the sums of those who see it
+                // through a probability of zero: zeros instead, and NaN in the sums of those who see it.  Nor may the scale of a page of which
+                // no row sees anything, or of page 0 in the place of none: with 255 a zero is decoded to NaN
+                if (!any) v_scale = 127;
                 bool bad = false;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {

@@ -147,18 +147,20 @@ cache_prompt_kernel(CacheAttnArgs a)
                 *(v8bf*)(kbuf[buf] + key * KROW + ((2 * d16 + e) ^ shift) * 16) = decode8<E5M2>(cd.k[u][2 * e], cd.k[u][2 * e + 1], sc);
         }
         // Where not all rows see all positions: values that no row sees may be anything, and a NaN among the others must not reach the
-        // rows that do not see it through a probability of zero.  Zeros instead; NaN is put into the sums of those who see it below.
+        // rows that do not see it through a probability of zero.  Zeros instead; NaN is put into the sums of those who see it below.  Nor may
+        // the scale that zeros are decoded with be anything, where the page is missing or no row sees any of it: with 255 they become NaN.
         const bool open = pos + STEP - 1 <= wg_hi && (pos >= wg_lo || pos + STEP <= a.sinks);
         int odd = 0;
 #pragma unroll
         for (int u = 0; u < VCH; ++u) {
             const int ch = threadIdx.x + u * T, d = channel_of(ch);
-            const float sc = __int_as_float(cd.vsc[UNI ? 0 : u] << 23);
+            float sc = __int_as_float(cd.vsc[UNI ? 0 : u] << 23);
             const bool there = cd.there[UNI ? 0 : u];
             if (!there) odd |= 1 << (ch & 3);
             if (!open || !there) {
                 auto below = [&](int q) { return (1u << min(max(q - pos - (ch & 3) * 16, 0), 16)) - 1u; };
                 const unsigned seen = there ? below(any_hi + 1) & (~below(any_lo) | below(a.sinks)) : 0u;
+                if (!seen) sc = 1.f;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     cd.v[u][w] &= bytes_of(seen >> (4 * w));

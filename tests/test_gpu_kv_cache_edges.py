@@ -1,0 +1,88 @@
+"""The paged 8-bit key / value cache where its pages, scales and lengths end: scale bytes that nobody should see, pages that are missing
+between others."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_03950_amd import binding as dma
+from test_gpu_kv_cache import Pair, bf16, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    dma.load()
+
+
+def compare(pair, q, start, n=None, window=0, sinks=0):
+    """Every row that exists against the definition, NaN for NaN; the others left as they were."""
+    B, _, N, _ = q.shape
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    got = dma.dma_cache_attn(q.cuda(), pair.gpu, i32(start), i32(n), window=window, sink_tokens=sinks, out=out).double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want, bound = pair.cpu.attn(q.double().numpy(), start, n, window, sinks)
+    count = np.full(B, N) if n is None else np.clip(n, 0, N)
+    exists = (np.arange(N) < np.where(np.asarray(start) < 0, 0, count)[:, None])[:, None, :, None] & np.ones(q.shape, bool)
+    assert (got[~exists] == 7).all()
+    np.testing.assert_array_equal(np.isnan(got[exists]), np.isnan(want[exists]))
+    fine = exists & ~np.isnan(want)
+    assert (np.abs(got - want)[fine] <= bound[fine]).all(), np.nanmax((np.abs(got - want) / bound)[fine])
+    return want, exists
+
+
+# ------------------------------------------------------------------------------- what lies where nothing has been written
+# rows per kv head: 4, 25 and 48 (one and two tiles of the kernel for few rows), 160
+ROWS = [(1, 4), (5, 5), (3, 16), (40, 4)]
+
+
+@pytest.mark.parametrize("N,G", ROWS)
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("fmt,D,P", [("e4m3", 128, 16), ("e5m2", 64, 32), ("e4m3", 64, 64), ("e5m2", 128, 64), ("e4m3", 128, 256)])
+def test_scales_that_nobody_should_see(fmt, D, P, wide, N, G):
+    """The scale of every page that nothing was written to is 255, the byte of no number: page 0, which no table names and which entries
+    without a page must not be mistaken for, pages handed out beyond the last token, and a page missing in the middle."""
+    rng = np.random.default_rng(N + D + P)
+    lens = [N, 3 * P, 2 * P + 63, 300, P + 40 if P < 256 else 300]
+    used = [-(-n // P) for n in lens]
+    order, at = 1 + rng.permutation(sum(used) + 3 * len(lens)), 0
+    table = np.full((len(lens), max(used) + 3 + (2048 // P if wide else 0)), -1, np.int32)
+    for b, u in enumerate(used):
+        table[b, :u + 3] = order[at:at + u + 3]
+        at += u + 3
+    table[2, 1] = -1
+    table[3, 300 // P - 1 if P < 256 else 0] = 1 << 30
+    pair = Pair(rng, None, 2, P, D, fmt, table, 1 + len(order))
+    pair.gpu.k_scales.fill_(255)
+    pair.gpu.v_scales.fill_(255)
+    S = max(lens)
+    pair.write(bf16(rng, len(lens), 2, S, D), bf16(rng, len(lens), 2, S, D), [0] * len(lens), lens)
+    q = bf16(rng, len(lens), 2 * G, N, D)
+    for window, sinks in ((0, 0), (70, 5)):
+        want, exists = compare(pair, q, np.array(lens) - N, None, window, sinks)
+        assert not np.isnan(want[exists]).any()
+
+
+@pytest.mark.parametrize("N,G", ROWS)
+@pytest.mark.parametrize("fmt,D,P", [("e4m3", 64, 16), ("e5m2", 128, 32), ("e4m3", 128, 64), ("e5m2", 64, 128), ("e4m3", 64, 256)])
+def test_pages_missing_between_others(fmt, D, P, N, G):
+    """Steps with a page and steps without, in any order, among them rows that see nothing at all."""
+    rng = np.random.default_rng(N + P)
+    lens, Hkv = [700, 700, 513, 700], 2
+    wide = -(-700 // P)
+    table = rng.permutation(4 * wide).reshape(4, wide).astype(np.int32)
+    table[0, ::2] = -1
+    table[1, 1:-1] = -1
+    table[2, :] = -1                                            # nothing anywhere
+    table[3, -2:] = 4 * wide
+    pair = Pair(rng, None, Hkv, P, D, fmt, table, 4 * wide)
+    pair.gpu.k_scales.fill_(255)
+    pair.gpu.v_scales.fill_(255)
+    pair.write(bf16(rng, 4, Hkv, 700, D), bf16(rng, 4, Hkv, 700, D), [0] * 4, lens)
+    q = bf16(rng, 4, Hkv * G, N, D)
+    for start in (np.array(lens) - N, np.array([0, P - 1, 2 * P, 333])):
+        for window, sinks in ((0, 0), (90, 3)):
+            want, exists = compare(pair, q, start, None, window, sinks)
+            assert not want[2].any()
