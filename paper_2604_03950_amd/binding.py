@@ -272,10 +272,11 @@ class KVCache:
     @classmethod
     def empty(cls, page_table: torch.Tensor, num_pages: int, Hkv: int, D: int, page_tokens: int = 64,
               fmt: int = FMT_MXFP8_E4M3) -> "KVCache":
-        """A cache of num_pages pages that hold nothing yet, on page_table's GPU."""
+        """A cache of num_pages pages that hold nothing yet (scales of 255), on page_table's GPU.  A page that is handed to another
+        sequence holds nothing again once its scales are 255; one that is written from its first position on needs no such thing."""
         mk = lambda *shape: torch.empty(shape, dtype=torch.uint8, device=page_table.device)
-        return cls(mk(num_pages, Hkv, page_tokens, D), mk(num_pages, Hkv, D, page_tokens), mk(num_pages, Hkv), mk(num_pages, Hkv),
-                   page_table, fmt)
+        none = lambda: torch.full((num_pages, Hkv), 255, dtype=torch.uint8, device=page_table.device)
+        return cls(mk(num_pages, Hkv, page_tokens, D), mk(num_pages, Hkv, D, page_tokens), none(), none(), page_table, fmt)
 
 
 _BF16, _I32 = torch.bfloat16, torch.int32

@@ -180,13 +180,14 @@ kv_write_kernel(CacheView c, Rows k, Rows v, Spans s, int pages_per_seq)
     __shared__ unsigned wave_top[16];
     top = __float_as_uint(cross_half_max(row_pair_max(group_max<16>(__uint_as_float(top << 16))))) >> 16;
     if ((threadIdx.x & 63) == 0) wave_top[threadIdx.x >> 6] = top;
-    const int before = it.lo ? *scale_at : 0;                   // every thread reads it before one replaces it
+    int before = it.lo ? *scale_at : 0;                         // every thread reads it before one replaces it
+    if (before < CACHE_SCALE_MIN || before > cache_scale_max(E5M2)) before = 0;       // no write left it: the page holds nothing
     __syncthreads();
     for (int i = 0; i < (int)blockDim.x >> 6; ++i) top = max(top, wave_top[i]);
     // the smallest scale that holds it: 1.75 * 2^n and less have significand bits up to 96 of 128
     const int need = min(max((int)((top + 31) >> 7) - EMAX, CACHE_SCALE_MIN), cache_scale_max(E5M2));
     const int scale = max(need, before);
-    const bool grown = it.lo && scale > before;
+    const bool grown = before && scale > before;
     const float down = __int_as_float((127 - min(scale - before, 100)) << 23);
     if (threadIdx.x == 0) *scale_at = (uint8_t)scale;
     if (!active) return;

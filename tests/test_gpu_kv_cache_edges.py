@@ -1,11 +1,12 @@
 """The paged 8-bit key / value cache where its pages, scales and lengths end: scale bytes that nobody should see, pages that are missing
-between others."""
+between others, writes into pages that hold nothing."""
 import numpy as np
 import pytest
 import torch
 
+import kv_plain as plain
 from paper_2604_03950_amd import binding as dma
-from test_gpu_kv_cache import Pair, bf16, i32
+from test_gpu_kv_cache import FMT, Pair, bf16, i32, table_of
 
 pytestmark = pytest.mark.gpu
 
@@ -63,6 +64,41 @@ def test_scales_that_nobody_should_see(fmt, D, P, wide, N, G):
     for window, sinks in ((0, 0), (70, 5)):
         want, exists = compare(pair, q, np.array(lens) - N, None, window, sinks)
         assert not np.isnan(want[exists]).any()
+
+
+@pytest.mark.parametrize("byte", [0, 16, 247, 255])
+@pytest.mark.parametrize("fmt,P,D", [("e4m3", 16, 64), ("e5m2", 64, 128), ("e4m3", 256, 128)])
+def test_written_from_the_middle(fmt, P, D, byte):
+    """A first write that starts inside a page whose scale no write has left: the page holds nothing, and takes its scale from the new
+    tokens alone; the next ones go on from there."""
+    rng = np.random.default_rng(P + byte)
+    pair = Pair(rng, [P + 9] * 3, 2, P, D, fmt)
+    pair.gpu.k_scales.fill_(byte)
+    pair.gpu.v_scales.fill_(byte)
+    pair.cpu.ks[...] = pair.cpu.vs[...] = 0
+    start = np.array([5, P - 1, 1])
+    for n, size in ((3, 1.0), (1, 2.0 ** 9), (2, 2.0 ** -7)):
+        pair.write(bf16(rng, 3, 2, n, D) * size, bf16(rng, 3, 2, n, D) / size, start)
+        pair.same()
+        start = start + n
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_empty_cache_holds_nothing(fmt):
+    """A new cache's memory is that of tensors freed before it; its pages hold nothing all the same."""
+    rng = np.random.default_rng(3)
+    Hkv, P, D = 2, 32, 64
+    table, pages = table_of(rng, [40, 40], P)
+    for byte in (255, 200, 1):
+        freed = [torch.full((pages, Hkv), byte, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        del freed
+        cache = dma.KVCache.empty(torch.from_numpy(table).cuda(), pages, Hkv, D, P, FMT[fmt])
+        k, v = bf16(rng, 2, Hkv, 4, D), bf16(rng, 2, Hkv, 4, D)
+        dma.dma_kv_write(cache, k.cuda(), v.cuda(), i32([7, 20]))
+        for b in range(2):
+            for h in range(Hkv):
+                assert int(cache.k_scales[table[b, 0], h]) == plain.needed(float(k[b, h].abs().max()), fmt)
+                assert int(cache.v_scales[table[b, 0], h]) == plain.needed(float(v[b, h].abs().max()), fmt)
 
 
 @pytest.mark.parametrize("N,G", ROWS)
