@@ -220,6 +220,9 @@ typedef struct dma_rows {
  *   B >= 0, N >= 0 (0 is a no-op).  N < 2^30.
  *   start      [B] int32, device, 4-byte aligned.  A sequence with a negative start has no tokens.
  *   n_tokens   [B] int32, device, 4-byte aligned, or NULL: N for every sequence.  Counts outside [0, N] are clamped to it.
+ *   A call whose launch would need 2^32 threads and more is refused (DMA_ERR_UNSUPPORTED).  Write and read: 2 * B * Hkv * (pages that
+ *   N tokens can touch) * max(64, page_tokens * D / 32) of them.  Attention: never with B * Hkv * ceil(N * Hq / Hkv / 32) < 2^19;
+ *   and query rows, B * Hq * N, are counted up to 2^30.
  * start, n_tokens and the page table are read by the kernels, so a captured graph follows their values from replay to replay.
  */
 

@@ -569,6 +569,10 @@ static int64_t reach_of(const CacheView& c, int rows, int G, int window, int sin
 // chip's other CUs save (one sequence of 1000, 8 kv heads: 10.6 us as one kernel).
 constexpr int64_t SHORT_REACH = 20 * STEP;
 
+// Workgroups per item of the join, and whether a launch can hold the items' threads.
+static int64_t join_groups(int rows, int G, int N) { return std::min<int64_t>(rows / 4, ((int64_t)N * G + 3) / 4); }
+static bool few_fit(int64_t items, int64_t threads_per_item) { return items <= 0xffffffffLL / threads_per_item; }
+
 size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window, int sinks)
 {
     const int G = Hq / c.Hkv;
@@ -576,6 +580,7 @@ size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window
     const int mt = mt_of(G, N), rows = 16 * mt;
     if (reach_of(c, rows, G, window, sinks) <= SHORT_REACH) return 0;
     const int64_t tiles = ((int64_t)N * G + rows - 1) / rows, items = (int64_t)B * c.Hkv * tiles;
+    if (!few_fit(items, join_groups(rows, G, N) * 1024)) return 0;
     return (size_t)(2 * grid_of(waves_of(mt, items)) * rows * (c.D + 2) * 4 + items * 8);
 }
 
@@ -584,13 +589,16 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
 {
     constexpr int ROWS = 16 * MT;
     const int64_t tiles = ((int64_t)a.s.N * a.G + ROWS - 1) / ROWS, items = (int64_t)a.s.B * a.c.Hkv * tiles;
-    if (items * (ROWS / 4) * 1024 > 0xffffffffLL) return DMA_ERR_UNSUPPORTED_;
     a.row_tiles = (int)tiles;
     const bool uni = a.c.page_shift >= 6;
-    if (reach_of(a.c, ROWS, a.G, a.window, a.sinks) <= SHORT_REACH)
+    if (reach_of(a.c, ROWS, a.G, a.window, a.sinks) <= SHORT_REACH) {
+        if (!few_fit(items, 512)) return DMA_ERR_UNSUPPORTED_;
         return uni ? launch(cache_attn_kernel<D, E5M2, MT, 8, true, true>, dim3((unsigned)items), dim3(512), stream, a)
                    : launch(cache_attn_kernel<D, E5M2, MT, 8, true, false>, dim3((unsigned)items), dim3(512), stream, a);
-    // the units of the line are counted in 31 bits
+    }
+    const int64_t join_y = join_groups(ROWS, a.G, a.s.N);
+    if (!few_fit(items, join_y * 1024)) return DMA_ERR_UNSUPPORTED_;
+    // the units of the line are counted in 31 bits (at most 2^22 items: some shift suffices)
     while (items * ((a.capacity / STEP >> a.unit_shift) + 2) > 0x7fffffff) ++a.unit_shift;
     const int waves = waves_of(MT, items);
     const int64_t grid = grid_of(waves);
@@ -602,7 +610,7 @@ static int launch_few(CacheAttnArgs a, void* workspace, hipStream_t stream)
     };
     const int rc = waves == 8 ? go(IC<8>{}) : go(IC<4>{});
     if (rc != DMA_OK_) return rc;
-    return launch(cache_attn_join_kernel<D, ROWS>, dim3((unsigned)items, (unsigned)std::min<int64_t>(ROWS / 4, ((int64_t)a.s.N * a.G + 3) / 4)), dim3(1024), stream, a);
+    return launch(cache_attn_join_kernel<D, ROWS>, dim3((unsigned)items, (unsigned)join_y), dim3(1024), stream, a);
 }
 
 int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const Spans& s, int Hq, int window, int sinks,

@@ -1,5 +1,5 @@
 """The paged 8-bit key / value cache where its pages, scales and lengths end: scale bytes that nobody should see, pages that are missing
-between others, writes into pages that hold nothing."""
+between others, writes into pages that hold nothing, batches of a million."""
 import numpy as np
 import pytest
 import torch
@@ -122,3 +122,22 @@ def test_pages_missing_between_others(fmt, D, P, N, G):
         for window, sinks in ((0, 0), (90, 3)):
             want, exists = compare(pair, q, start, None, window, sinks)
             assert not want[2].any()
+
+
+# ------------------------------------------------------------------------------------------------------------- batches
+@pytest.mark.parametrize("B,G", [(1 << 20, 1), (1 << 19, 20)])
+@pytest.mark.parametrize("pages", [1, 81])
+def test_a_million_sequences(B, G, pages):
+    """Sequences of one token, with a table that holds little and one that may hold long ones: each sees its own key alone."""
+    D, P, held = 64, 16, 1000
+    table = torch.full((B, pages), -1, dtype=torch.int32, device="cuda")
+    table[:, 0] = torch.arange(B, device="cuda") % held
+    cache = dma.KVCache.empty(table, held, 1, D, P)
+    first = dma.KVCache(cache.k_codes, cache.v_codes, cache.k_scales, cache.v_scales, table[:held].contiguous())
+    k, v = (torch.randn((held, 1, 1, D), device="cuda").to(torch.bfloat16) for _ in range(2))
+    zeros = torch.zeros(B, dtype=torch.int32, device="cuda")
+    dma.dma_kv_write(first, k, v, zeros[:held])
+    v = dma.dma_kv_read(first, zeros[:held], 1)[1]
+    out = dma.dma_cache_attn(k[:1].expand(B, G, 1, D), cache, zeros)
+    for at in range(0, B, 1 << 16):
+        assert torch.equal(out[at:at + (1 << 16)], v[torch.arange(at, at + (1 << 16), device="cuda") % held].expand(-1, G, -1, -1)), at
