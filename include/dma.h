@@ -205,7 +205,8 @@ typedef struct dma_kv_cache {
 
 /* A bf16 tensor [B, heads, N, D] whose rows of D elements are dense and lie where the strides (in elements) say: token n of
  * head h of sequence b starts at data + b * stride_batch + h * stride_head + n * stride_token.  data is 16-byte aligned and
- * the strides are multiples of 8 (both so that a row can be read 16 bytes at a time) and not negative. */
+ * the strides are multiples of 8 (both so that a row can be read 16 bytes at a time) and not negative.  Rows that a call reads may
+ * lie in the same place (a stride of 0 repeats them); those that it writes must not: a stride of 0 over more than one is refused. */
 typedef struct dma_rows {
     void* data;
     int64_t stride_batch;

@@ -283,7 +283,8 @@ _BF16, _I32 = torch.bfloat16, torch.int32
 
 
 def _rows(t: torch.Tensor, what: str, shape, index: int) -> _Rows:
-    """A bf16 tensor [B, heads, N, D] whose rows are dense, at any strides the library takes (it checks them)."""
+    """A bf16 tensor [B, heads, N, D] whose rows are dense, at any strides the library takes (it checks them; an expanded tensor is read and
+    not written)."""
     if t.dtype is not _BF16 or t.get_device() != index or t.shape != shape:
         raise ValueError(f"{what}: need a torch.bfloat16 tensor {tuple(shape)} on the cache's GPU")
     sb, sh, sn, sd = t.stride()

@@ -76,6 +76,15 @@ int check_rows(const dma_rows* r, dma::Rows& out)
     return DMA_OK;
 }
 
+// ... of rows that are written: a stride of 0 would put different rows in the same place.
+int check_out_rows(const dma_rows* r, int B, int heads, int N, dma::Rows& out)
+{
+    const int rc = check_rows(r, out);
+    if (rc != DMA_OK) return rc;
+    if ((B > 1 && r->stride_batch == 0) || (heads > 1 && r->stride_head == 0) || (N > 1 && r->stride_token == 0)) return DMA_ERR_INVALID_ARG;
+    return DMA_OK;
+}
+
 // Query rows and work items of the attention over the cache are counted in 32 bits.
 bool attn_sizes_fit(int B, int Hq, int Hkv, int N)
 {
@@ -236,7 +245,7 @@ int dma_kv_read(const dma_kv_cache* cache, const dma_rows* k_out, const dma_rows
     int rc = check_cache(cache, B, N, c);
     if (rc != DMA_OK || B == 0 || N == 0) return rc;
     if ((rc = check_spans(start_i32, n_tokens_i32, B, N, s)) != DMA_OK) return rc;
-    if ((rc = check_rows(k_out, rk)) != DMA_OK || (rc = check_rows(v_out, rv)) != DMA_OK) return rc;
+    if ((rc = check_out_rows(k_out, B, c.Hkv, N, rk)) != DMA_OK || (rc = check_out_rows(v_out, B, c.Hkv, N, rv)) != DMA_OK) return rc;
     return dma::launch_kv_read(c, rk, rv, s, (hipStream_t)stream);
 }
 
@@ -251,7 +260,7 @@ int dma_cache_attn(const dma_kv_cache* cache, const dma_rows* q, const dma_rows*
     if (Hq <= 0 || Hq % c.Hkv != 0 || window < 0 || sink_tokens < 0) return DMA_ERR_INVALID_ARG;
     if (B == 0 || N == 0) return DMA_OK;
     if ((rc = check_spans(start_i32, n_tokens_i32, B, N, s)) != DMA_OK) return rc;
-    if ((rc = check_rows(q, rq)) != DMA_OK || (rc = check_rows(out, ro)) != DMA_OK) return rc;
+    if ((rc = check_rows(q, rq)) != DMA_OK || (rc = check_out_rows(out, B, Hq, N, ro)) != DMA_OK) return rc;
     if (!attn_sizes_fit(B, Hq, c.Hkv, N)) return DMA_ERR_UNSUPPORTED;
     const size_t need = dma::cache_attn_workspace(c, B, Hq, N, window, sink_tokens);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return DMA_ERR_INVALID_ARG;
