@@ -100,7 +100,8 @@ DMA_DEV int pack_bf16(float a, float b)
     return __builtin_bit_cast(int, r);
 }
 
-// Bytes that are no number (NaN, infinity): bit 7 of each.
+// Bytes that are no number (NaN, infinity): bit 7 of each.  Both are put into the sums as NaN where a step is masked; in the others an
+// infinity goes through the products as one.
 template <bool E5M2>
 DMA_DEV unsigned no_number(unsigned w) { return ((w & 0x7f7f7f7fu) + (E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u; }
 

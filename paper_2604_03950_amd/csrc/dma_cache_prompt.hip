@@ -4,7 +4,8 @@
 // them, and all walk the same steps of 64 positions.  The codes of a step are decoded to bf16 once per workgroup, into LDS (exact: the
 // page's scale is applied), one step ahead of their use; one barrier per step.  As in the kernel for few rows, S^T = K Q^T takes its key
 // rows in an order that leaves every probability in the lane that needs it for O^T = V^T P^T, and the softmax's maximum is raised only
-// where the sum of a lane's 32 probabilities exceeds 1024.
+// where the sum of a lane's 32 probabilities exceeds 1024.  Probabilities are rounded to bf16 as there, for the same reason; here a second term of
+// theirs would lengthen by half the products that bound the kernel.
 //
 // Measured, 32 query and 8 kv heads, D = 128: 2048 tokens behind 14k 545 to 590 us = 0.87 to 0.95 PFLOP/s, 4096 behind 28k 0.98 (a bf16 matrix product
 // of 8192^3 runs at 1.15 here); 512 behind 7.5k 91 us = 0.73; 8192 under a window of 1024 180 to 205 us, 0.63 to 0.72 of the visible pairs' flops.  Two

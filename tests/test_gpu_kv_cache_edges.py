@@ -1,5 +1,6 @@
 """The paged 8-bit key / value cache where its pages, scales and lengths end: scale bytes that nobody should see, pages that are missing
-between others, writes into pages that hold nothing, batches of a million."""
+between others, writes into pages that hold nothing, infinities and large values, batches of a
+million."""
 import numpy as np
 import pytest
 import torch
@@ -122,6 +123,46 @@ def test_pages_missing_between_others(fmt, D, P, N, G):
         for window, sinks in ((0, 0), (90, 3)):
             want, exists = compare(pair, q, start, None, window, sinks)
             assert not want[2].any()
+
+
+# ------------------------------------------------------------------------------------------------------ not a number
+@pytest.mark.parametrize("N,G", ROWS)
+@pytest.mark.parametrize("P", [16, 64])
+def test_infinities_of_others(P, N, G):
+    """E5M2 codes of infinities, which no write leaves: not finite in the channels of the rows that see one, nothing for the rest."""
+    rng = np.random.default_rng(N + P)
+    S, D = 200, 64
+    pair = Pair(rng, [S, S], 1, P, D, "e5m2")
+    pair.write(bf16(rng, 2, 1, S, D), bf16(rng, 2, 1, S, D), [0, 0])
+    for b, t, d, code in ((0, S - N + N // 2, 5, 0x7c), (0, 60, 9, 0xfc), (1, S - 1, 63, 0xfc)):
+        page, u = pair.cpu.place(b, t)
+        pair.cpu.v[page, 0, d, u] = code
+        pair.gpu.v_codes[page, 0, d, u] = code
+    q = bf16(rng, 2, G, N, D)
+    for window in (0, 30):
+        got = dma.dma_cache_attn(q.cuda(), pair.gpu, i32([S - N] * 2), window=window).double().cpu().numpy()
+        with np.errstate(invalid="ignore"):
+            want, bound = pair.cpu.attn(q.double().numpy(), [S - N] * 2, None, window)
+        fine = np.isfinite(want)                                # the definition's table has NaN for an infinity
+        np.testing.assert_array_equal(np.isfinite(got), fine)
+        assert not fine.all() and (np.abs(got - want) <= bound)[fine].all()
+
+
+# --------------------------------------------------------------------------------------------------------- magnitudes
+@pytest.mark.parametrize("N,G", ROWS)
+def test_large_values(N, G):
+    """Values up to 2^121 / (512 + 64), the largest whose sums are said to stay in binary32, with scores that rise from key to key so that
+    the running maximum stays behind."""
+    rng = np.random.default_rng(N)
+    S, D = 512, 64
+    pair = Pair(rng, [S], 1, 64, D, "e4m3")
+    k, v = bf16(rng, 1, 1, S, D) * 0.01, (1 + bf16(rng, 1, 1, S, D).abs().clamp(max=0.9).double()) * 2.0 ** 110
+    k[0, 0, :, 0] = torch.arange(S) // 8                       # base 2: 16 / 8 * log2(e) / 8 = 0.36 from a group of 8 keys to the next
+    pair.write(k.to(torch.bfloat16), v.to(torch.bfloat16), [0])
+    q = bf16(rng, 1, G, N, D) * 0.01
+    q[..., 0] = 2.0
+    want, _ = compare(pair, q.to(torch.bfloat16), [S - N])
+    assert np.isfinite(want).all()
 
 
 # ------------------------------------------------------------------------------------------------------------- batches
