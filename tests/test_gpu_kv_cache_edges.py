@@ -1,11 +1,12 @@
 """The paged 8-bit key / value cache where its pages, scales and lengths end: scale bytes that nobody should see, pages that are missing
-between others, writes into pages that hold nothing, infinities and large values, batches of a
+between others, writes into pages that hold nothing, NaN over all kinds of pages, infinities and large values, every key counted, batches of a
 million."""
 import numpy as np
 import pytest
 import torch
 
 import kv_plain as plain
+from kv_counts import channel, counts, wrong
 from paper_2604_03950_amd import binding as dma
 from test_gpu_kv_cache import FMT, Pair, bf16, i32, table_of
 
@@ -126,6 +127,26 @@ def test_pages_missing_between_others(fmt, D, P, N, G):
 
 
 # ------------------------------------------------------------------------------------------------------ not a number
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2, 0), (70, 0), (20, 41)])
+@pytest.mark.parametrize("B,Hkv,G,N", [(2, 1, 4, 3), (2, 1, 2, 20), (2, 2, 2, 100)])
+@pytest.mark.parametrize("fmt,D,P", [("e4m3", 64, 16), ("e5m2", 128, 16), ("e5m2", 64, 32), ("e4m3", 128, 32), ("e4m3", 64, 64), ("e5m2", 128, 128), ("e5m2", 64, 256),
+                                     ("e4m3", 128, 256)])
+def test_nan_over_all_kinds_of_pages(fmt, D, P, B, Hkv, G, N, window, sinks):
+    """A NaN key or value reaches the queries that see it, under a window and among the sinks too, and no others."""
+    rng = np.random.default_rng(N + P + D)
+    S = 300
+    pair = Pair(rng, [S] * B, Hkv, P, D, fmt)
+    k, v = bf16(rng, B, Hkv, S, D), bf16(rng, B, Hkv, S, D)
+    nan = float("nan")
+    v[0, 0, S - N + N // 2, 5] = v[0, 0, S - N + N // 2, D - 1] = v[0, 0, 40, 33] = nan
+    v[1, 0, S - N - 1, 17] = v[1, 0, S - 1, 6] = nan
+    k[1, Hkv - 1, S - max(N // 2, 1), 3] = nan
+    pair.write(k, v, [0] * B)
+    pair.same()
+    want, exists = compare(pair, bf16(rng, B, Hkv * G, N, D), [S - N] * B, None, window, sinks)
+    assert np.isnan(want).any() and not np.isnan(want).all()
+
+
 @pytest.mark.parametrize("N,G", ROWS)
 @pytest.mark.parametrize("P", [16, 64])
 def test_infinities_of_others(P, N, G):
@@ -146,6 +167,62 @@ def test_infinities_of_others(P, N, G):
         fine = np.isfinite(want)                                # the definition's table has NaN for an infinity
         np.testing.assert_array_equal(np.isfinite(got), fine)
         assert not fine.all() and (np.abs(got - want) <= bound)[fine].all()
+
+
+# ------------------------------------------------------------------------------------------------------- every key once
+# few rows with eight waves and with four, in one tile and in two; many rows in pieces and whole; B, Hkv, G, N, the longest
+SHAPES = [(1, 2, 4, 1, 4000), (40, 4, 2, 1, 3000), (1, 2, 8, 4, 4000), (2, 2, 5, 12, 2000), (70, 4, 8, 3, 2500), (1, 2, 4, 40, 4000), (70, 4, 2, 70, 1500),
+          (3, 2, 4, 1, 1200)]
+
+
+def counting_cache(rng, lens, Hkv, P, D, fmt, wide=0):
+    """Values of one in one channel of every position, kv heads by turns in either pattern."""
+    table, pages = table_of(rng, lens, P)
+    if wide:
+        big = torch.full((len(lens), wide), -1, dtype=torch.int32, device="cuda")
+        big[:, :table.shape[1]] = torch.from_numpy(table).cuda()
+    cache = dma.KVCache.empty(big if wide else torch.from_numpy(table).cuda(), pages, Hkv, D, P, FMT[fmt])
+    S = max(lens)
+    t = torch.arange(S, device="cuda")
+    v = torch.zeros((1, Hkv, S, D), dtype=torch.bfloat16, device="cuda")
+    for h in range(Hkv):
+        v[0, h, t, channel(t, D, h & 1)] = 1
+    k = torch.randn((1, Hkv, S, D), device="cuda").to(torch.bfloat16)
+    dma.dma_kv_write(cache, k.expand(len(lens), -1, -1, -1), v.expand(len(lens), -1, -1, -1), i32([0] * len(lens)), i32(lens))
+    return cache
+
+
+def count_all(cache, G, N, start, window, sinks):
+    B, Hkv, D = cache.B, cache.Hkv, cache.D
+    q = torch.zeros((B, Hkv * G, N, D), dtype=torch.bfloat16, device="cuda")
+    got = dma.dma_cache_attn(q, cache, i32(start), window=window, sink_tokens=sinks)
+    got = got.view(B, Hkv // 2, 2, G, N, D)
+    assert (got == got[:, :1, :, :1]).all()                     # heads of a pattern are alike
+    got = got[:, 0, :, 0].double().cpu().numpy()                # [B, 2, N, D]
+    for b in range(B):
+        for i in range(N):
+            count, n = counts(D, int(start[b]) + i, window, sinks)
+            assert not wrong(got[b, :, i], count, n).any(), (b, i, int(start[b]) + i)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 70), (1300, 5)])
+@pytest.mark.parametrize("fmt,D,P", [("e4m3", 128, 64), ("e5m2", 64, 16), ("e4m3", 64, 256), ("e5m2", 128, 32)])
+@pytest.mark.parametrize("B,Hkv,G,N,longest", SHAPES)
+def test_every_key_counts_once(B, Hkv, G, N, longest, fmt, D, P, window, sinks):
+    rng = np.random.default_rng(B + N + P + window)
+    lens = np.concatenate([[longest, 1300 if longest > 1300 else N, 1281 if longest > 1300 else 65, longest - 63][:B], rng.integers(N, longest, max(B - 4, 0))])
+    lens = np.maximum(lens, N)
+    cache = counting_cache(rng, list(lens), Hkv, P, D, fmt)
+    count_all(cache, G, N, lens - N, window, sinks)
+
+
+@pytest.mark.parametrize("N", [1, 12])
+def test_every_key_counts_once_in_a_line_of_coarse_units(N):
+    """More than 2^31 steps by the sizes alone: the line of steps is cut in units of several."""
+    rng = np.random.default_rng(N)
+    lens = list(rng.integers(N, 3000, 64))
+    cache = counting_cache(rng, lens, 2, 256, 128, "e4m3", wide=(1 << 22) - 1)
+    count_all(cache, 2, N, np.array(lens) - N, 0, 0)
 
 
 # --------------------------------------------------------------------------------------------------------- magnitudes
