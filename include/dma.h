@@ -234,11 +234,12 @@ typedef struct dma_rows {
  * (e_max = 8 for E4M3, 15 for E5M2: the largest element is 1.75 * 2^e_max, so no finite element saturates), but at least 17
  * and at most 246 (E4M3) or 239 (E5M2): every element times its scale is then a normal bf16 number or zero.  Elements are
  * rounded to nearest even; an infinity becomes the largest element, a NaN stays one.
- * A page whose first written position is not its first one holds earlier tokens, if its scale is one that a write leaves (17 and
- * more, at most 246 or 239; any other byte, 255 for one, says that the page holds nothing, and the positions before the tokens are not written): its scale stays where it suffices for the new
- * tokens.  Where it does not, the scale grows and the earlier codes are rounded once more, to element * 2^(old - new) (exact
- * but for what becomes subnormal).  A page that is written from its first position on takes its scale from the new tokens alone,
- * whatever it held.  What a page holds behind the last token written is not kept.
+ * A page whose first written position is not its first one holds earlier tokens if its scale is one that a write leaves (17 to 246,
+ * or to 239; any other byte, 255 for one, says that the page holds nothing, and the places before the tokens stay as they
+ * are).  Its scale then stays where it suffices for the new tokens.  Where it does not, the scale grows and the earlier codes are
+ * rounded once more, to element * 2^(old - new) (exact but for what becomes subnormal).  A page that is written from its first
+ * position on takes its scale from the new tokens alone, whatever it held.  What a page holds behind the last token written is
+ * not kept.
  * Positions past max_pages * page_tokens are dropped.  Two sequences that write to the same page in one call: unspecified.
  */
 int dma_kv_write(const dma_kv_cache* cache, const dma_rows* k, const dma_rows* v, int B, int N, const void* start_i32,

@@ -27,17 +27,26 @@ HIPCC_FLAGS = [
 ]
 
 
-def source_digest() -> str:
-    """SHA-256 over the sources of the forward and the quantizers and the public header (file names and contents, sorted by
-    name): what a profile summary records so that a figure measured on one version of the kernels is not quoted for another."""
+def _digest(names: list[str]) -> str:
+    """SHA-256 over the named sources and the public header (file names and contents, sorted by name): what a profile summary
+    records so that a figure measured on one version of the kernels is not quoted for another."""
     import hashlib
     h = hashlib.sha256()
-    names = sorted(n for n in os.listdir(CSRC) if n.endswith((".hip", ".hpp")) and not n.startswith("dma_cache"))
-    for path in [os.path.join(CSRC, n) for n in names] + [os.path.join(HERE, "..", "include", "dma.h")]:
+    for path in [os.path.join(CSRC, n) for n in sorted(names)] + [os.path.join(HERE, "..", "include", "dma.h")]:
         h.update(os.path.basename(path).encode() + b"\0")
         with open(path, "rb") as f:
             h.update(f.read())
     return h.hexdigest()
+
+
+def source_digest() -> str:
+    """The digest of the forward and the quantizers."""
+    return _digest([n for n in os.listdir(CSRC) if n.endswith((".hip", ".hpp")) and not n.startswith("dma_cache")])
+
+
+def cache_digest() -> str:
+    """The digest of the key / value cache's kernels and what they include."""
+    return _digest([n for n in os.listdir(CSRC) if n.startswith("dma_cache")] + ["dma_device.hpp", "dma_internal.hpp"])
 
 
 def _stale(obj: str, deps: list[str]) -> bool:
@@ -83,5 +92,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
 if __name__ == "__main__":
     if "--digest" in sys.argv:
         print(source_digest())
+    elif "--cache-digest" in sys.argv:
+        print(cache_digest())
     else:
         print(build(force="--incremental" not in sys.argv, verbose="-v" in sys.argv))

@@ -572,7 +572,8 @@ static int64_t reach_of(const CacheView& c, int rows, int G, int window, int sin
     return window ? std::min(capacity, (int64_t)window + std::min(sinks, 1 << 30) + rows / G + 3 * STEP) : capacity;
 }
 // One workgroup per item, eight waves of it, where no item is longer than this: a second kernel to join pieces costs more than the
-// chip's other CUs save (one sequence of 1000, 8 kv heads: 10.6 us as one kernel).
+// chip's other CUs save (one sequence of 1000, 8 kv heads: 10.0 us as one kernel, 11.8 with the shares and the join).  What counts is
+// the reach of the table, as the lengths are on the device: under a table for 32k the sequence of 1000 takes the 11.8.
 constexpr int64_t SHORT_REACH = 20 * STEP;
 
 // Workgroups per item of the join, and whether a launch can hold the items' threads.

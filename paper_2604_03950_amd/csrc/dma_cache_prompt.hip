@@ -7,7 +7,7 @@
 // where the sum of a lane's 32 probabilities exceeds 1024.  Probabilities are rounded to bf16 as there, for the same reason; here a second term of
 // theirs would lengthen by half the products that bound the kernel.
 //
-// Measured, 32 query and 8 kv heads, D = 128: 2048 tokens behind 14k 545 to 590 us = 0.87 to 0.95 PFLOP/s, 4096 behind 28k 0.98 (a bf16 matrix product
+// Measured, 32 query and 8 kv heads, D = 128: 2048 tokens behind 14k 530 to 590 us = 0.87 to 0.97 PFLOP/s, 4096 behind 28k 0.98 (a bf16 matrix product
 // of 8192^3 runs at 1.15 here); 512 behind 7.5k 91 us = 0.73; 8192 under a window of 1024 180 to 205 us, 0.63 to 0.72 of the visible pairs' flops.  Two
 // workgroups of four waves per CU: while one waits at the barrier the other's products run; matrix and vector time of a SIMD add up otherwise.
 #include "dma_cache_device.hpp"
