@@ -352,7 +352,8 @@ def dma_cache_attn(q: torch.Tensor, cache: KVCache, start: torch.Tensor, n_token
     """q [B, Hq, N, D] bf16 (any strides with dense rows), token i of sequence b at position start[b] + i, attends to the
     cache's keys at and before its own position (window > 0: to the last `window` of them and the first sink_tokens positions)
     -> out [B, Hq, N, D] bf16.  Rows that do not exist (behind n_tokens, or of a sequence with a
-    negative start) are left as they were in out; without out they are zeros.
+    negative start) are left as they were in out; without out they are zeros (a launch more: 12.1 us instead of 10.0 for a token
+    behind 1000).
     workspace: contiguous uint8 of at least dma_cache_attn_workspace_bytes(...) bytes, for one call at a time; by default one
     is allocated."""
     stream = _cache_stream(cache)

@@ -6,7 +6,7 @@
 // innermost).  A whole page's values go through LDS, where they are turned, and cross memory in one piece.
 //
 // Bound by memory.  Measured at 32 kv heads x 8192 tokens, D = 128, written (134 MB read, 67 written): 34.4 us = 5.9 TB/s; 8 kv heads x 32768 read
-// back: 30.2 us = 6.7 TB/s (a copy of as many bytes 32.5).  One token of 8 kv heads: 4.6 us, one chain of loads.
+// back: 30.2 us = 6.7 TB/s (a copy of as many bytes 32.5).  One token of 8 kv heads: 4.8 us, one chain of loads.
 #include "dma_cache_device.hpp"
 #include <algorithm>
 

@@ -12,9 +12,9 @@
 // (16 positions of a lane have p of 1024 together at most), in binary32 for every value below 2^121 / (n + 64).
 //
 // p is rounded to bf16 because the matrix instruction takes both operands in one type, and bf16 is the one that decoded values fit without
-// rounding (their exponents do not fit binary16).  It costs 2^-8 of the weighted mean of |v| and |o| at most; against 64 bits the listed
-// kinds of calls are 0.0019 to 0.0021 off (relative, over all elements), with unrounded p 0.0016 to 0.0017: the result's own rounding to bf16.  p in
-// two bf16 terms would take the second product twice.
+// rounding (their exponents do not fit binary16).  It costs 2^-8 of the weighted mean of |v| and |o| at most; over 1k to 32k keys the results
+// are 0.0017 to 0.0021 from those in 64 bits (relative, over all elements), with unrounded p 0.0016 to 0.0017: their own rounding to bf16.  p in two
+// bf16 terms would take the second product twice.
 //
 // Long and uneven sequences: the steps of all (sequence, kv head, row tile) items form one line that is cut into equal shares, one
 // per workgroup.  An item that lies in one share is written directly; pieces of the others go to the workspace, and a second
