@@ -278,6 +278,68 @@ int dma_cache_attn(const dma_kv_cache* cache, const dma_rows* q, const dma_rows*
  * 0 also for arguments that the call refuses. */
 size_t dma_cache_attn_workspace_bytes(const dma_kv_cache* cache, int B, int Hq, int N, int window, int sink_tokens);
 
+/*
+ * Pages that several sequences hold, and who holds what.
+ *
+ * Rows of the page table may name the same page.  refs [num_pages] int32 (device, 4-byte aligned) says of every page how many entries of
+ * the table name it; a page of which it says 0 is free.  A caller that begins with a table of -1 and refs of 0 and changes both only by the
+ * three calls below has them in line.  They write the page table of the cache, although the structure holds it as a pointer to
+ * const, and they read and write the table's first B rows only.  Their work on the table and on refs is exact and does not depend on the order in which threads run.  Calls that
+ * change the same table or refs have to follow one another.  With refs that do not count the table's entries the results are unspecified
+ * (never a fault, as long as B and the sizes are those of the buffers).
+ *
+ * dma_kv_fork: row b of the table becomes the first ceil(length[b] / page_tokens) entries that row src[b] had before the call, and -1 behind
+ * them.  Nothing is copied but entries; a sequence that goes on to write into a page it shares calls dma_kv_reserve first.
+ *   src_i32     [B] int32, device, 4-byte aligned.  Outside [0, B): the row becomes empty.  b itself: the row keeps its first entries.
+ *   length_i32  [B] int32, device, 4-byte aligned: positions that are kept, up to the table's width; below 1 none.  NULL: whole rows.
+ *   So: beams in a new order (src = their origins), samples of one prompt (src = its row, length = its tokens), drafts taken back (src = b and
+ *   a shorter length), sequences that end (src = -1).
+ *   B > 16384: DMA_ERR_UNSUPPORTED.
+ */
+int dma_kv_fork(const dma_kv_cache* cache, void* refs_i32, int B, const void* src_i32, const void* length_i32, void* stream);
+
+/*
+ * Makes the pages of positions [start[b], start[b] + n_tokens[b]) the sequence's own, so that dma_kv_write can write them: an entry that is no
+ * page, or a page with refs > 1, becomes a free page; the r-th of these entries, sequence by sequence and in order of position, the r-th
+ * free page in ascending order (refs as they were before the call say what is shared and what is free).  Where the sequence has earlier
+ * tokens in a shared page (its first one, start not a multiple of page_tokens), the codes and scales of the whole page are copied; any other
+ * page that is handed out holds nothing (scales of 255).  Every sequence that shares a page it asks for leaves it; none keeps it.
+ *   start, n_tokens, N   as for dma_kv_write; positions past max_pages * page_tokens are none.
+ *   missing_i32  [B] int32, device, 4-byte aligned, out: entries of the sequence for which no free page was left.  They stay as they were,
+ *                and what is written to them would be lost, or be written to a page of others.
+ *   workspace    device, 4-byte aligned, at least dma_kv_reserve_workspace_bytes(...) bytes; as for dma_cache_attn.
+ *   B times the pages that N tokens can touch must stay below 2^30 (else DMA_ERR_UNSUPPORTED).
+ */
+int dma_kv_reserve(const dma_kv_cache* cache, void* refs_i32, int B, int N, const void* start_i32, const void* n_tokens_i32, void* missing_i32,
+                   void* workspace, size_t workspace_bytes, void* stream);
+size_t dma_kv_reserve_workspace_bytes(const dma_kv_cache* cache, int B, int N);
+
+/*
+ * Brings the pages in use (refs > 0) to the first places: with U of them, the i-th page in use from U on moves, codes and scales, to the
+ * i-th free one below U, both in ascending order.  refs and the entries of the table's B rows follow.
+ *   used_i32   [1] int32, device, 4-byte aligned, out: U.
+ *   moved_i32  [num_pages] int32, device, 4-byte aligned, out: where the page lies now, -1 for free ones (what a caller needs for other
+ *              tables of page numbers).
+ *   workspace  device, 8-byte aligned, at least dma_kv_compact_workspace_bytes(...) bytes; as for dma_cache_attn.
+ */
+int dma_kv_compact(const dma_kv_cache* cache, void* refs_i32, int B, void* used_i32, void* moved_i32, void* workspace, size_t workspace_bytes,
+                   void* stream);
+size_t dma_kv_compact_workspace_bytes(const dma_kv_cache* cache);
+
+/*
+ * dma_cache_attn for sequences that share a long prefix, whose keys and values are read once for all of them.
+ *   n_groups >= 0; group_start [n_groups + 1] int32, device, 4-byte aligned, not decreasing: group g holds the sequences group_start[g] up to
+ *   group_start[g + 1] (not included), of the B.  A sequence may be in no group.
+ *   shared [n_groups] int32, device, 4-byte aligned: the positions [0, shared[g]) of all sequences of group g are the same: their rows of the table
+ *   name the same pages there (or pages that hold the same).  What is read for all is read by the first row of the group.
+ *   Everything else is as for dma_cache_attn, and so is what the call computes; the order of its sums differs, and so may the last bits.
+ * A group_start that decreases gives unspecified results, never a fault.  With n_groups = 0 the two arrays are not looked at (may be NULL).
+ */
+int dma_cache_attn_shared(const dma_kv_cache* cache, const dma_rows* q, const dma_rows* out, int B, int Hq, int N, const void* start_i32,
+                          const void* n_tokens_i32, int n_groups, const void* group_start_i32, const void* shared_i32, int window, int sink_tokens,
+                          void* workspace, size_t workspace_bytes, void* stream);
+size_t dma_cache_attn_shared_workspace_bytes(const dma_kv_cache* cache, int B, int Hq, int N, int n_groups, int window, int sink_tokens);
+
 /* Diagnostic, not part of the method: plain device-to-device copy kernel (16 bytes per lane, no reuse) of `bytes`
  * bytes (a multiple of 16; src, dst 16-byte aligned, device, non-overlapping).  Its exactly known traffic (bytes read +
  * bytes written) is what the HBM byte counters of a profiler run are scaled by. */

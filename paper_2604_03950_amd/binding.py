@@ -18,7 +18,9 @@ FMT_MXFP4_E2M1 = 2
 FMT_MXFP8_E5M2 = 3
 
 EXPORTS = ("dma_mx_quantize", "dma_mx_quantize_token", "dma_mx_quantize_dual", "dma_mx_group_amax", "dma_attn_fwd", "dma_attn_fwd_ex",
-           "dma_attn_fwd_workspace_bytes", "dma_kv_write", "dma_kv_read", "dma_cache_attn", "dma_cache_attn_workspace_bytes", "dma_diag_copy", "dma_diag_mfma", "dma_diag_pipes", "dma_error_string", "dma_version")
+           "dma_attn_fwd_workspace_bytes", "dma_kv_write", "dma_kv_read", "dma_cache_attn", "dma_cache_attn_workspace_bytes",
+           "dma_kv_fork", "dma_kv_reserve", "dma_kv_reserve_workspace_bytes", "dma_kv_compact", "dma_kv_compact_workspace_bytes", "dma_cache_attn_shared",
+           "dma_cache_attn_shared_workspace_bytes", "dma_diag_copy", "dma_diag_mfma", "dma_diag_pipes", "dma_error_string", "dma_version")
 
 PIPE_IDLE, PIPE_MFMA_BF16, PIPE_MFMA_FP4, PIPE_MFMA_FP8, PIPE_FMA, PIPE_EXP, PIPE_CVT_PK_BF16 = range(7)
 
@@ -83,6 +85,20 @@ def load() -> ctypes.CDLL:
         L.dma_cache_attn.argtypes = [pc, pr, pr, ci, ci, ci, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
         L.dma_cache_attn_workspace_bytes.restype = ctypes.c_size_t
         L.dma_cache_attn_workspace_bytes.argtypes = [pc, ci, ci, ci, ci, ci]
+        L.dma_kv_fork.restype = ci
+        L.dma_kv_fork.argtypes = [pc, vp, ci, vp, vp, vp]
+        L.dma_kv_reserve.restype = ci
+        L.dma_kv_reserve.argtypes = [pc, vp, ci, ci, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.dma_kv_reserve_workspace_bytes.restype = ctypes.c_size_t
+        L.dma_kv_reserve_workspace_bytes.argtypes = [pc, ci, ci]
+        L.dma_kv_compact.restype = ci
+        L.dma_kv_compact.argtypes = [pc, vp, ci, vp, vp, vp, ctypes.c_size_t, vp]
+        L.dma_kv_compact_workspace_bytes.restype = ctypes.c_size_t
+        L.dma_kv_compact_workspace_bytes.argtypes = [pc]
+        L.dma_cache_attn_shared.restype = ci
+        L.dma_cache_attn_shared.argtypes = [pc, pr, pr, ci, ci, ci, vp, vp, ci, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
+        L.dma_cache_attn_shared_workspace_bytes.restype = ctypes.c_size_t
+        L.dma_cache_attn_shared_workspace_bytes.argtypes = [pc, ci, ci, ci, ci, ci, ci]
         L.dma_diag_copy.restype = ci
         L.dma_diag_copy.argtypes = [vp, vp, i64, vp]
         L.dma_diag_mfma.restype = ci
@@ -389,6 +405,128 @@ def dma_cache_attn(q: torch.Tensor, cache: KVCache, start: torch.Tensor, n_token
 def dma_cache_attn_workspace_bytes(cache: KVCache, Hq: int, N: int, window: int = 0, sink_tokens: int = 0) -> int:
     """Bytes of workspace of a dma_cache_attn call with q [B, Hq, N, D] on the current device."""
     return int(load().dma_cache_attn_workspace_bytes(cache._ref, cache.B, Hq, N, window, sink_tokens))
+
+
+def _ints(cache: KVCache, t: torch.Tensor, n: int, what: str) -> int:
+    if t.dtype is not _I32 or t.get_device() != cache._index or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what}: need a contiguous torch.int32 tensor [{n}] on the cache's GPU")
+    return t.data_ptr()
+
+
+def _scratch(cache: KVCache, workspace: torch.Tensor | None, need: int):
+    """(pointer, bytes) of a call's workspace, allocated where the caller has none, and what keeps it alive."""
+    if workspace is None:
+        if not need:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+        return workspace.data_ptr(), need, workspace
+    if workspace.get_device() != cache._index:
+        raise ValueError("workspace: need it on the cache's GPU")
+    return _dev(workspace, torch.uint8, "workspace"), workspace.numel(), workspace
+
+
+def dma_kv_fork(cache: KVCache, refs: torch.Tensor, src: torch.Tensor, length: torch.Tensor | None = None) -> None:
+    """Row b of the cache's page table becomes the entries that hold the first length[b] positions (all by default) of what row src[b]
+    was before; src[b] outside [0, B): nothing.  refs: int32 [pages] on the GPU, the entries that name each page, 0 for free pages
+    (all of them for a new cache, whose table is -1); src, length: int32 [B]."""
+    stream = _cache_stream(cache)
+    pr = _ints(cache, refs, cache._c.num_pages, "refs")
+    ps = _counts(cache, src, "src")
+    pl = None if length is None else _counts(cache, length, "length")
+    rc = load().dma_kv_fork(cache._ref, pr, cache.B, ps, pl, stream)
+    if rc:
+        raise DmaError(rc, "dma_kv_fork")
+
+
+def dma_kv_reserve(cache: KVCache, refs: torch.Tensor, start: torch.Tensor, N: int, n_tokens: torch.Tensor | None = None, *,
+                   missing: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Makes the pages of positions start[b] + [0, n_tokens[b]) (N of them by default) the sequence's own, before they are written: free pages
+    where it has none or shares them, with the earlier tokens of a shared page copied.  Returns missing, int32 [B]: entries of each
+    sequence for which no free page was left.  workspace: contiguous uint8 of at least dma_kv_reserve_workspace_bytes(...) bytes, for one
+    call at a time; by default one is allocated."""
+    stream = _cache_stream(cache)
+    pr = _ints(cache, refs, cache._c.num_pages, "refs")
+    ps = _counts(cache, start, "start")
+    pn = None if n_tokens is None else _counts(cache, n_tokens, "n_tokens")
+    if not -1 << 31 <= N < 1 << 31:
+        raise ValueError("N must be an int of 32 bits")
+    if missing is None:
+        missing = torch.zeros(cache._b, dtype=_I32, device=cache.device)
+    pm = _counts(cache, missing, "missing")
+    L = load()
+    pw, nw, workspace = _scratch(cache, workspace, 0 if workspace is not None else L.dma_kv_reserve_workspace_bytes(cache._ref, cache.B, N))
+    rc = L.dma_kv_reserve(cache._ref, pr, cache.B, N, ps, pn, pm, pw, nw, stream)
+    if rc:
+        raise DmaError(rc, "dma_kv_reserve")
+    return missing
+
+
+def dma_kv_reserve_workspace_bytes(cache: KVCache, N: int) -> int:
+    """Bytes of workspace of a dma_kv_reserve call for N tokens."""
+    return int(load().dma_kv_reserve_workspace_bytes(cache._ref, cache.B, N))
+
+
+def dma_kv_compact(cache: KVCache, refs: torch.Tensor, *, used: torch.Tensor | None = None, moved: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None):
+    """Moves the pages in use to the first places of the cache; its table and refs follow.  Returns (used, moved): int32 [1], how many there are,
+    and int32 [pages], where each page lies now (-1: free).  workspace: contiguous uint8 of at least
+    dma_kv_compact_workspace_bytes(cache) bytes, 8-byte aligned, for one call at a time; by default one is allocated."""
+    stream = _cache_stream(cache)
+    pages = cache._c.num_pages
+    pr = _ints(cache, refs, pages, "refs")
+    if used is None:
+        used = torch.zeros(1, dtype=_I32, device=cache.device)
+    if moved is None:
+        moved = torch.empty(pages, dtype=_I32, device=cache.device)
+    pu, pm = _ints(cache, used, 1, "used"), _ints(cache, moved, pages, "moved")
+    L = load()
+    pw, nw, workspace = _scratch(cache, workspace, 0 if workspace is not None else L.dma_kv_compact_workspace_bytes(cache._ref))
+    rc = L.dma_kv_compact(cache._ref, pr, cache.B, pu, pm, pw, nw, stream)
+    if rc:
+        raise DmaError(rc, "dma_kv_compact")
+    return used, moved
+
+
+def dma_kv_compact_workspace_bytes(cache: KVCache) -> int:
+    """Bytes of workspace of a dma_kv_compact call."""
+    return int(load().dma_kv_compact_workspace_bytes(cache._ref))
+
+
+def dma_cache_attn_shared(q: torch.Tensor, cache: KVCache, start: torch.Tensor, groups: torch.Tensor, shared: torch.Tensor,
+                          n_tokens: torch.Tensor | None = None, *, window: int = 0, sink_tokens: int = 0, out: torch.Tensor | None = None,
+                          workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """dma_cache_attn for sequences with common prefixes, each of which is read once: the sequences groups[g] .. groups[g + 1] - 1 have the
+    same pages for their first shared[g] positions (int32 [n + 1], not decreasing, and int32 [n], on the GPU).  Everything else as there."""
+    stream = _cache_stream(cache)
+    ps = _counts(cache, start, "start")
+    pn = None if n_tokens is None else _counts(cache, n_tokens, "n_tokens")
+    if shared.dim() != 1:
+        raise ValueError("shared must be [n], groups [n + 1]")
+    n_groups = shared.shape[0]
+    pg, psh = _ints(cache, groups, n_groups + 1, "groups"), _ints(cache, shared, n_groups, "shared")
+    if q.dim() != 4:
+        raise ValueError("q must be [B, Hq, N, D]")
+    B, index = cache.B, cache._index
+    _, Hq, N, _ = q.shape
+    shape = (B, Hq, N, cache.D)
+    rq = _rows(q, "q", shape, index)
+    if out is None:
+        out = torch.zeros(shape, dtype=_BF16, device=cache.device)
+    ro = _rows(out, "out", shape, index)
+    if not (0 <= window < 1 << 31 and 0 <= sink_tokens < 1 << 31):
+        raise ValueError("window and sink_tokens must be in [0, 2^31)")
+    L = load()
+    pw, nw, workspace = _scratch(cache, workspace, 0 if workspace is not None else
+                                 L.dma_cache_attn_shared_workspace_bytes(cache._ref, B, Hq, N, n_groups, window, sink_tokens))
+    rc = L.dma_cache_attn_shared(cache._ref, rq, ro, B, Hq, N, ps, pn, n_groups, pg, psh, window, sink_tokens, pw, nw, stream)
+    if rc:
+        raise DmaError(rc, "dma_cache_attn_shared")
+    return out
+
+
+def dma_cache_attn_shared_workspace_bytes(cache: KVCache, Hq: int, N: int, n_groups: int, window: int = 0, sink_tokens: int = 0) -> int:
+    """Bytes of workspace of a dma_cache_attn_shared call with q [B, Hq, N, D] and n_groups groups on the current device."""
+    return int(load().dma_cache_attn_shared_workspace_bytes(cache._ref, cache.B, Hq, N, n_groups, window, sink_tokens))
 
 
 def dma_diag_copy(src: torch.Tensor, dst: torch.Tensor) -> None:

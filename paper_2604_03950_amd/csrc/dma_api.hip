@@ -91,6 +91,11 @@ bool attn_sizes_fit(int B, int Hq, int Hkv, int N)
     return (int64_t)N * (Hq / Hkv) <= 1 << 30 && (int64_t)B * Hq <= (1 << 30) / N;
 }
 
+// refs counts the entries of a table that can be written; a cache without pages has none to count.
+bool check_refs(const dma::CacheView& c, const void* refs) { return c.num_pages == 0 || (refs && aligned4(refs)); }
+
+bool reserve_fits(const dma::CacheView& c, int B, int N) { return dma::reserve_pages(c, N) * B < (int64_t)1 << 30; }
+
 }  // namespace
 
 static int quantize_one(const void* x_bf16, int64_t rows, int D, int fmt, int is_query, void* codes_u8,
@@ -272,6 +277,85 @@ size_t dma_cache_attn_workspace_bytes(const dma_kv_cache* cache, int B, int Hq, 
     dma::CacheView c;
     if (check_cache_sizes(cache, B, N, c) != DMA_OK || B == 0 || N == 0 || Hq <= 0 || Hq % c.Hkv != 0 || window < 0 || sink_tokens < 0) return 0;
     return attn_sizes_fit(B, Hq, c.Hkv, N) ? dma::cache_attn_workspace(c, B, Hq, N, window, sink_tokens) : 0;
+}
+
+int dma_kv_fork(const dma_kv_cache* cache, void* refs_i32, int B, const void* src_i32, const void* length_i32, void* stream)
+{
+    dma::CacheView c;
+    const int rc = check_cache(cache, B, 1, c);
+    if (rc != DMA_OK || B == 0) return rc;
+    if (!check_refs(c, refs_i32) || !src_i32 || !aligned4(src_i32) || !aligned4(length_i32)) return DMA_ERR_INVALID_ARG;
+    if (B > dma::FORK_ROWS_MAX) return DMA_ERR_UNSUPPORTED;
+    return dma::launch_kv_fork(c, (int*)refs_i32, B, (const int*)src_i32, (const int*)length_i32, (hipStream_t)stream);
+}
+
+int dma_kv_reserve(const dma_kv_cache* cache, void* refs_i32, int B, int N, const void* start_i32, const void* n_tokens_i32, void* missing_i32,
+                   void* workspace, size_t workspace_bytes, void* stream)
+{
+    dma::CacheView c;
+    dma::Spans s;
+    int rc = check_cache(cache, B, N, c);
+    if (rc != DMA_OK || B == 0 || N == 0) return rc;
+    if ((rc = check_spans(start_i32, n_tokens_i32, B, N, s)) != DMA_OK) return rc;
+    if (!check_refs(c, refs_i32) || !missing_i32 || !aligned4(missing_i32)) return DMA_ERR_INVALID_ARG;
+    if (!reserve_fits(c, B, N)) return DMA_ERR_UNSUPPORTED;
+    const size_t need = dma::reserve_pages(c, N) * B * 4;
+    if (need && (!workspace || !aligned4(workspace) || workspace_bytes < need)) return DMA_ERR_INVALID_ARG;
+    return dma::launch_kv_reserve(c, (int*)refs_i32, s, (int*)missing_i32, (int*)workspace, (hipStream_t)stream);
+}
+
+size_t dma_kv_reserve_workspace_bytes(const dma_kv_cache* cache, int B, int N)
+{
+    dma::CacheView c;
+    if (check_cache_sizes(cache, B, N, c) != DMA_OK || B == 0 || N == 0 || !reserve_fits(c, B, N)) return 0;
+    return dma::reserve_pages(c, N) * B * 4;
+}
+
+int dma_kv_compact(const dma_kv_cache* cache, void* refs_i32, int B, void* used_i32, void* moved_i32, void* workspace, size_t workspace_bytes,
+                   void* stream)
+{
+    dma::CacheView c;
+    const int rc = check_cache(cache, B, 1, c);
+    if (rc != DMA_OK || B == 0) return rc;
+    if (!check_refs(c, refs_i32) || !used_i32 || !aligned4(used_i32)) return DMA_ERR_INVALID_ARG;
+    if (c.num_pages > 0 && (!moved_i32 || !aligned4(moved_i32))) return DMA_ERR_INVALID_ARG;
+    const size_t need = dma::compact_workspace(c);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7u) != 0 || workspace_bytes < need) return DMA_ERR_INVALID_ARG;
+    return dma::launch_kv_compact(c, (int*)refs_i32, B, (int*)used_i32, (int*)moved_i32, workspace, (hipStream_t)stream);
+}
+
+size_t dma_kv_compact_workspace_bytes(const dma_kv_cache* cache)
+{
+    dma::CacheView c;
+    return check_cache_sizes(cache, 1, 1, c) == DMA_OK ? dma::compact_workspace(c) : 0;
+}
+
+int dma_cache_attn_shared(const dma_kv_cache* cache, const dma_rows* q, const dma_rows* out, int B, int Hq, int N, const void* start_i32,
+                          const void* n_tokens_i32, int n_groups, const void* group_start_i32, const void* shared_i32, int window, int sink_tokens,
+                          void* workspace, size_t workspace_bytes, void* stream)
+{
+    dma::CacheView c;
+    dma::Spans s;
+    dma::Rows rq, ro;
+    int rc = check_cache(cache, B, N, c);
+    if (rc != DMA_OK) return rc;
+    if (Hq <= 0 || Hq % c.Hkv != 0 || window < 0 || sink_tokens < 0 || n_groups < 0) return DMA_ERR_INVALID_ARG;
+    if (B == 0 || N == 0) return DMA_OK;
+    if ((rc = check_spans(start_i32, n_tokens_i32, B, N, s)) != DMA_OK) return rc;
+    if ((rc = check_rows(q, rq)) != DMA_OK || (rc = check_out_rows(out, B, Hq, N, ro)) != DMA_OK) return rc;
+    if (n_groups > 0 && (!group_start_i32 || !shared_i32 || !aligned4(group_start_i32) || !aligned4(shared_i32))) return DMA_ERR_INVALID_ARG;
+    if (!attn_sizes_fit(B, Hq, c.Hkv, N) || n_groups > 1 << 24) return DMA_ERR_UNSUPPORTED;
+    const size_t need = dma::cache_attn_shared_workspace(c, B, Hq, N, n_groups, window, sink_tokens);
+    if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return DMA_ERR_INVALID_ARG;
+    const dma::Groups groups = {(const int*)group_start_i32, (const int*)shared_i32, n_groups};
+    return dma::launch_cache_attn_shared(c, rq, ro, s, Hq, groups, window, sink_tokens, workspace, (hipStream_t)stream);
+}
+
+size_t dma_cache_attn_shared_workspace_bytes(const dma_kv_cache* cache, int B, int Hq, int N, int n_groups, int window, int sink_tokens)
+{
+    dma::CacheView c;
+    if (check_cache_sizes(cache, B, N, c) != DMA_OK || B == 0 || N == 0 || Hq <= 0 || Hq % c.Hkv != 0 || window < 0 || sink_tokens < 0 || n_groups < 0 || n_groups > 1 << 24) return 0;
+    return attn_sizes_fit(B, Hq, c.Hkv, N) ? dma::cache_attn_shared_workspace(c, B, Hq, N, n_groups, window, sink_tokens) : 0;
 }
 
 int dma_diag_copy(const void* src, void* dst, int64_t bytes, void* stream)

@@ -88,4 +88,22 @@ int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const 
                       void* workspace, hipStream_t stream);
 size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window, int sinks);
 
+// Pages that several sequences hold (dma_cache_pages.hip).  refs: table entries per page.
+constexpr int FORK_ROWS_MAX = 16384;
+int launch_kv_fork(const CacheView& c, int* refs, int B, const int* src, const int* length, hipStream_t stream);
+int launch_kv_reserve(const CacheView& c, int* refs, const Spans& s, int* missing, int* workspace, hipStream_t stream);
+int64_t reserve_pages(const CacheView& c, int N);          // that N tokens can touch
+int launch_kv_compact(const CacheView& c, int* refs, int B, int* used, int* moved, void* workspace, hipStream_t stream);
+size_t compact_workspace(const CacheView& c);
+
+// Sequences first[g] .. first[g + 1] - 1 share their positions below shared[g].
+struct Groups {
+    const int* first;
+    const int* shared;
+    int n;
+};
+int launch_cache_attn_shared(const CacheView& c, const Rows& q, const Rows& out, const Spans& s, int Hq, const Groups& groups, int window, int sinks,
+                             void* workspace, hipStream_t stream);
+size_t cache_attn_shared_workspace(const CacheView& c, int B, int Hq, int N, int n_groups, int window, int sinks);
+
 }  // namespace dma
