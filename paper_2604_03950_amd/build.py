@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdma_mi355x.so")
 SOURCES = ["dma_api.hip", "dma_quantize.hip", "dma_attn_fwd.hip", "dma_cache.hip", "dma_cache_attn.hip", "dma_cache_prompt.hip", "dma_cache_pages.hip", "dma_cache_shared.hip",
            "dma_diag.hip"]
-HEADERS = ["dma_device.hpp", "dma_plan.hpp", "dma_internal.hpp", "dma_attn_kernel.hpp", "dma_attn_split.hpp", "dma_cache_device.hpp", "dma_cache_few.hpp", "dma_cache_many.hpp",
+HEADERS = ["dma_device.hpp", "dma_plan.hpp", "dma_internal.hpp", "dma_attn_kernel.hpp", "dma_attn_split.hpp", "dma_cache_device.hpp", "dma_cache_many.hpp",
            os.path.join("..", "..", "include", "dma.h")]
 # (low, high) format pairs of the fused forward, as product-path ids of dma_device.hpp: dma_attn_inst.hip is compiled
 # once per pair (the list mirrors the declarations in dma_attn_fwd.hip)

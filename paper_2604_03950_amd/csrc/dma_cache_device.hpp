@@ -35,7 +35,6 @@ DMA_DEV int scalar_at(const int* table, int index)
 
 struct SeqInfo {
     int start, n;
-    int own;                 // the first step that is the sequence's own, where those before are shared
 };
 DMA_DEV SeqInfo seq_of(const CacheAttnArgs& a, int b)
 {
@@ -50,29 +49,22 @@ DMA_DEV SeqInfo seq_of(const CacheAttnArgs& a, int b)
 template <bool FEW>
 DMA_DEV int token_of(const CacheAttnArgs& a, int row) { return FEW ? (int)((unsigned)row * a.inv_g >> 16) : row / a.G; }
 
-// The steps that a row tile visits: [base, base + sink_steps) and [first, first + steps - sink_steps).
+// The steps that a row tile visits: [0, sink_steps) and [first, first + steps - sink_steps).  ONE: a sequence has one tile.
 struct StepRange {
-    int sink_steps, first, steps, base;
-    DMA_DEV int position(int j) const { return (j < sink_steps ? base + j : first + j - sink_steps) * STEP; }
+    int sink_steps, first, steps;
+    DMA_DEV int position(int j) const { return (j < sink_steps ? j : first + j - sink_steps) * STEP; }
 };
-// ONE: a sequence has one tile.  OWN: only steps from q.own on.
-template <int ROWS, bool ONE, bool OWN = false>
+template <int ROWS, bool ONE>
 DMA_DEV StepRange range_of(const CacheAttnArgs& a, const SeqInfo& q, int tile)
 {
     const int64_t from = (int64_t)q.start + (ONE ? 0 : tile * ROWS / a.G), to = (int64_t)q.start + (ONE ? q.n - 1 : min(q.n - 1, (tile * ROWS + ROWS - 1) / a.G));
     const int hi = (int)min(to + 1, (int64_t)a.capacity);
     const int lo = a.window ? (int)min(max(from - a.window + 1, (int64_t)0), (int64_t)hi) : 0;
     StepRange r;
-    r.base = OWN ? q.own : 0;
-    r.first = OWN ? max(lo / STEP, r.base) : lo / STEP;
+    r.first = lo / STEP;
     r.sink_steps = (min(a.sinks, hi) + STEP - 1) / STEP;
-    if (OWN) r.sink_steps = max(r.sink_steps - r.base, 0);
-    if (r.base + r.sink_steps >= r.first) {
-        r.sink_steps = 0;
-        r.first = r.base;
-    }
+    if (r.sink_steps >= r.first) r.sink_steps = r.first = 0;
     r.steps = r.sink_steps + (hi + STEP - 1) / STEP - r.first;
-    if (OWN) r.steps = max(r.steps, 0);
     return r;
 }
 

@@ -3,10 +3,10 @@
 // softmax(q k^T) v over keys that lie in parts joins from the parts' maxima, weights and sums: m = max m_i, l = sum l_i 2^(m_i - m),
 // o = sum o_i 2^(m_i - m), out = o / l.  The shared part of a group (its positions below S = shared / 64 * 64, whole steps) is visited with
 // the rows of all its sequences in tiles of 128: a step's codes are read and decoded once for 128 rows, as for a piece of a prompt
-// (many_steps).  What a sequence has behind it is visited with its own rows, as for single tokens (few_rows).  One launch does both: the
+// (many_steps).  What a sequence has behind it is visited with its own rows in tiles of 16 or 32, a wave by itself to each tile, or to a part of its
+// steps: such parts are short, and waves that wait for each other would wait more than they work.  One launch does both: the
 // first is bound by matrix and vector work, the second by the bytes of the cache, and workgroups of both kinds share the CUs.  A second one
-// joins.  Nothing here knows how long the sequences are until it runs: each workgroup finds its part of the work by itself.
-#include "dma_cache_few.hpp"
+// joins.  How long the sequences are is on the device alone: each workgroup finds its part of the work by itself.
 #include "dma_cache_many.hpp"
 #include <algorithm>
 
@@ -17,13 +17,13 @@ constexpr int ROWS_MANY = 128;
 constexpr int WAVES = 4;
 
 struct SharedArgs {
-    CacheAttnArgs a;         // pieces and split: of what the sequences have to themselves
+    CacheAttnArgs a;         // pieces and split (first piece, how many): of what the sequences have to themselves, per tile of 16 * MT rows
     Groups g;
     int rows_per_seq;        // query rows of a kv head and sequence: N * G
     float* pieces;           // of the prefixes: per workgroup [128][D] sums, [128] maxima, [128] weights
-    int2* split;             // per item (kv head, row tile): the first piece and how many
-    int64_t max_pieces;
-    int resident;            // workgroups that the chip holds
+    int2* split;             // per kv head and row tile: the first piece and how many
+    int64_t max_pieces, max_own;
+    int more;                // workgroups beyond one for each row tile of a prefix and for four tiles of the sequences: items in several parts
 };
 
 struct Bounds {
@@ -55,25 +55,39 @@ DMA_DEV int group_of(const F& first, int n, int b)
     return lo > 0 && b < first(lo) ? lo - 1 : -1;
 }
 
-// What a sequence has to itself begins where its group's shared part ends.
-struct OwnBehindPrefix {
-    static constexpr bool ON = true;
-    const SharedArgs& x;
-    const int* first;        // in LDS, where there are few groups
-    const int* steps;
-    DMA_DEV SeqInfo seq(const CacheAttnArgs& a, int b) const
-    {
-        SeqInfo q = seq_of(a, b);
-        if (x.g.n <= GROUPS_LDS) {
-            const int g = group_of([&](int i) { return first[i]; }, x.g.n, b);
-            q.own = g < 0 ? 0 : steps[g];
-        } else {
-            const int g = group_of([&](int i) { return x.g.first[i]; }, x.g.n, b);
-            q.own = g < 0 ? 0 : shared_steps(x, x.g.shared[g]);
-        }
-        return q;
-    }
+// A sequence, and the first step that it does not share.
+struct OwnSeq {
+    int start, n, own;
 };
+
+// The steps that a row tile of a sequence visits behind what it shares: [own, own + sink_steps) and [first, first + steps - sink_steps).
+struct OwnRange {
+    int own, sink_steps, first, steps;
+    DMA_DEV int position(int j) const { return (j < sink_steps ? own + j : first + j - sink_steps) * STEP; }
+};
+template <int ROWS>
+DMA_DEV OwnRange own_range(const CacheAttnArgs& a, const OwnSeq& q, int tile)
+{
+    const int64_t from = (int64_t)q.start + tile * ROWS / a.G, to = (int64_t)q.start + min(q.n - 1, (tile * ROWS + ROWS - 1) / a.G);
+    const int hi = (int)min(to + 1, (int64_t)a.capacity);
+    const int lo = a.window ? (int)min(max(from - a.window + 1, (int64_t)0), (int64_t)hi) : 0;
+    OwnRange r;
+    r.own = q.own;
+    r.first = max(lo / STEP, q.own);
+    r.sink_steps = max((min(a.sinks, hi) + STEP - 1) / STEP - q.own, 0);
+    if (q.own + r.sink_steps >= r.first) {
+        r.sink_steps = 0;
+        r.first = q.own;
+    }
+    r.steps = max(r.sink_steps + (hi + STEP - 1) / STEP - r.first, 0);
+    return r;
+}
+
+// The same in all lanes, and known to be: what is derived from it takes scalar loads and branches.
+DMA_DEV int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
+}
 
 DMA_DEV int wave_scan(int x)                 // the sum up to and with this lane's
 {
@@ -138,7 +152,6 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     // ---- the steps: of the shared ones, those that a row sees
     const int hi = min(view.any_hi + 1, g.steps * STEP), lo = min(view.any_lo, hi);
     StepRange range;
-    range.base = 0;
     range.first = lo / STEP;
     range.sink_steps = (min(a.sinks, hi) + STEP - 1) / STEP;
     if (range.sink_steps >= range.first) range.sink_steps = range.first = 0;
@@ -162,93 +175,411 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     }
 }
 
-// What a step costs a workgroup: 64 positions for 128 rows of a prefix, and for one row tile of a sequence's own.
-constexpr int COST_MANY = 3, COST_FEW = 2;
+// One wave's part of what a sequence has to itself: steps [begin, end) for a tile of 16 * MT of its rows, into a piece.  S^T = K Q^T with the keys in
+// an order that leaves every probability in the lane that needs it for O^T = V^T P^T, one maximum per row that is raised only where it was far too
+// low, codes of the next step on their way while one is worked on: as in the kernel for few rows (dma_cache_attn.hip), whose comments say why.
+// qs: with 32 rows, room for the queries' operands in LDS.
+template <int D, bool E5M2, int MT, bool UNI>
+DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& range, int b, int h, int tile, int begin, int end, int64_t piece, v8bf* qs)
+{
+    constexpr int ROWS = 16 * MT, KJ = D / 64, DT = D / 16;
+    const CacheAttnArgs& a = x.a;
+    const CacheView& c = a.c;
+    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4, page_mask = (1 << c.page_shift) - 1;
+    const int rows = min(sq.n * a.G - tile * ROWS, ROWS);
+    const int* table = c.page_table + (int64_t)b * c.max_pages;
+    // ---- pages and codes of a step: of the 16 positions whose keys this lane loads, and of those whose values it loads
+    auto page_of = [&](int j, int g) -> int {
+        const int at = min((range.position(j) + (UNI ? 0 : 16 * g)) >> c.page_shift, c.max_pages - 1);
+        return UNI ? scalar_at(table, __builtin_amdgcn_readfirstlane(at)) : table[at];
+    };
+    auto there = [&](int page, int j, int g) -> int {             // looked at where it is used: looking at once would wait for the codes too
+        if constexpr (!UNI) asm volatile("" : "+v"(page));
+        return (range.position(j) + (UNI ? 0 : 16 * g)) >> c.page_shift < c.max_pages ? page : -1;
+    };
+    auto slab_of = [&](int page) -> int64_t {
+        if constexpr (UNI) page = __builtin_amdgcn_readfirstlane(page);
+        return (int64_t)((unsigned)page < c.page_limit ? page : 0) * c.Hkv + h;
+    };
+    v4i kr[4][KJ], vr[DT];
+    uint8_t k_scale = 0, v_scale = 0;
+    int v_page = -1;
+    // the positions of a lane's keys: 16 (col / 4) + 4 t + col % 4 in product t
+    auto load_k = [&](int j, int page, bool on) {
+        const int64_t slab = slab_of(page);
+        const int pos = range.position(j), at = 16 * (col >> 2);
+        const uint8_t* base = c.k_codes + ((slab << c.page_shift) + ((UNI ? pos : pos + at) & page_mask)) * D;
+        const uint8_t* p = base + (on ? (unsigned)(((UNI ? at : 0) + (col & 3)) * D + grp * 16) : 0u);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < KJ; ++i) kr[t][i] = *(const v4i*)(p + t * 4 * D + i * 64);
+        k_scale = c.k_scales[slab];
+    };
+    auto load_v = [&](int j, int page, bool on) {
+        const int64_t slab = slab_of(page);
+        const int pos = range.position(j);
+        const uint8_t* base = c.v_codes + ((slab * D) << c.page_shift) + ((UNI ? pos : pos + 16 * grp) & page_mask);
+        const unsigned mine = on ? (col << c.page_shift) + (UNI ? 16 * grp : 0) : 0u;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vr[dt] = *(const v4i*)(base + ((dt * 16) << c.page_shift) + mine);
+        v_scale = c.v_scales[slab];
+        v_page = page;
+    };
+    int pk = -1, pv = -1;                                         // pages of the step after the next
+    if (begin < end) {
+        pk = page_of(begin, col >> 2);
+        pv = UNI ? pk : page_of(begin, grp);
+    }
+    // ---- rows
+    v8bf qf[MT][2 * KJ];
+    int vis_lo[MT], vis_hi[MT];                                   // what the row of this lane's column sees: these positions and those below sinks
+    const int64_t from = sq.start;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = r / a.G;
+        const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + r - i * a.G) * a.q.stride_head + i * a.q.stride_token;
+#pragma unroll
+        for (int ks = 0; ks < 2 * KJ; ++ks) qf[mt][ks] = *(const v8bf*)(qp + ((ks >> 1) * 64 + grp * 16 + (ks & 1) * 8) * 2);
+        vis_hi[mt] = cut_position(from + i);
+        vis_lo[mt] = a.window ? cut_position(from + i - a.window + 1) : 0;
+    }
+    // ... and what all of them see
+    const int all_hi = cut_position(from + tile * ROWS / a.G), all_lo = a.window ? cut_position(from + (tile * ROWS + rows - 1) / a.G - a.window + 1) : 0;
+    __builtin_amdgcn_sched_barrier(0);
+    if (begin < end) {
+        const int page_v = there(pv, begin, grp);
+        load_k(begin, there(pk, begin, col >> 2), true);
+        pk = page_of(min(begin + 1, end - 1), col >> 2);
+        pv = UNI ? pk : page_of(min(begin + 1, end - 1), grp);
+        load_v(begin, page_v, true);
+    }
+    v4f o[MT][DT];
+    float m[MT], l[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[mt][dt] = v4f{0.f, 0.f, 0.f, 0.f};
+        m[mt] = M_NONE;
+        l[mt] = 0.f;
+        // the queries, requested first, have arrived before the loop: no wait for them inside it, which would be one for the codes
+#pragma unroll
+        for (int ks = 0; ks < 2 * KJ; ++ks) {
+            v4i w = __builtin_bit_cast(v4i, qf[mt][ks]);
+            asm volatile("" : "+v"(w));
+            if (MT == 1) qf[mt][ks] = __builtin_bit_cast(v8bf, w);
+            else qs[(mt * 2 * KJ + ks) * 64 + lane] = __builtin_bit_cast(v8bf, w);
+        }
+    }
+    for (int j = begin; j < end; ++j) {
+        // the codes of the next step are requested without a branch (what the compiler cannot count it waits for in full):
+        // behind the last step, one address for all lanes
+        const int next = min(j + 1, end - 1);
+        const bool more = j + 1 < end;
+        const int pos = range.position(j);
+        const bool page_ok = (unsigned)v_page < c.page_limit;
+        // ---- scores
+        v4f s[MT][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[mt][t] = v4f{0.f, 0.f, 0.f, 0.f};
+        const float ksc = __int_as_float(k_scale << 23);
+        int mine = lane;
+        if constexpr (MT > 1) {
+            asm volatile("" : "+v"(mine));                        // (so that they are not read once, before the loop, after all)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int ks = 0; ks < 2 * KJ; ++ks) qf[mt][ks] = qs[(mt * 2 * KJ + ks) * 64 + mine];
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int jj = 0; jj < KJ; ++jj)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const v8bf k = decode8<E5M2>(kr[t][jj][2 * e], kr[t][jj][2 * e + 1], ksc);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) s[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[mt][2 * jj + e], s[mt][t], 0, 0, 0);
+                }
+        // ---- the next step's keys, the pages of the one after it
+        const int page_v = there(pv, next, grp);
+        load_k(next, there(pk, next, col >> 2), more);
+        pk = page_of(min(j + 2, end - 1), col >> 2);
+        pv = UNI ? pk : page_of(min(j + 2, end - 1), grp);
+        // ---- what is not seen
+        const bool plain = pos + STEP - 1 <= all_hi && (pos >= all_lo || pos + STEP <= a.sinks) && __all(page_ok);
+        float y[MT][16];                                          // position 16 grp + 4 t + r of the step at 4 t + r
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[mt][e] = s[mt][e >> 2][e & 3];
+        if (!plain) {
+            unsigned any = 0;
+            const int base = pos + 16 * grp;
+            auto below = [&](int at) { return (1u << min(max(at - base, 0), 16)) - 1u; };
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                // bit e: the lane's 16 positions
+                const unsigned seen = page_ok ? below(vis_hi[mt] + 1) & (~below(vis_lo[mt]) | below(a.sinks)) : 0u;
+                any |= seen;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) y[mt][e] = (seen >> e) & 1u ? y[mt][e] : -INFINITY;
+            }
+            // over the rows: 16 columns hold different rows of the same positions
+            any |= __builtin_amdgcn_mov_dpp(any, 0x121, 0xF, 0xF, true);
+            any |= __builtin_amdgcn_mov_dpp(any, 0x122, 0xF, 0xF, true);
+            any |= __builtin_amdgcn_mov_dpp(any, 0x124, 0xF, 0xF, true);
+            any |= __builtin_amdgcn_mov_dpp(any, 0x128, 0xF, 0xF, true);
+            // values that no row sees may be anything, the scale of their page too, and a NaN among the others must not reach the rows that do
+            // not see it through a probability of zero: zeros instead, and NaN in the sums of those who see it
+            if (!any) v_scale = 127;
+            bool bad = false;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int keep = bytes_of(any >> (4 * w));
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    vr[dt][w] &= keep;
+                    const unsigned f = no_number<E5M2>((unsigned)vr[dt][w]);
+                    if (f) bad = true;
+                    vr[dt][w] &= (int)~((f >> 7) * 0xffu);
+                }
+            }
+            if (__any(bad)) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const unsigned long long hit = nan_channels<D, E5M2>(a, b, h, pos, vis_lo[mt], vis_hi[mt], D / 4, [&](int i) { return (i >> 2) * 16 + 4 * grp + (i & 3); });
+#pragma unroll
+                    for (int i = 0; i < D / 4; ++i) o[mt][i >> 2][i & 3] = (hit >> i) & 1 ? NAN : o[mt][i >> 2][i & 3];
+                }
+            }
+        }
+        // ---- softmax: the maximum is looked for only where it was too low, which the sum of a lane's 16 probabilities shows (a sum of the
+        // rounded ones, as the values' sums are)
+        v8bf pf[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            int pw[8];
+            float sum;
+            auto probabilities = [&] {
+                const float off = m[mt] * a.scale;
+                const v2bf one = __builtin_bit_cast(v2bf, 0x3f803f80);
+                float part[2] = {0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    pw[e] = pack_bf16(__builtin_amdgcn_exp2f(fmaf(y[mt][2 * e], a.scale, -off)), __builtin_amdgcn_exp2f(fmaf(y[mt][2 * e + 1], a.scale, -off)));
+                    part[e & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, pw[e]), one, part[e & 1], false);
+                }
+                sum = part[0] + part[1];
+            };
+            probabilities();
+            if (__any(sum > 1024.f)) {
+                float top = y[mt][0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) top = fmaxf(top, y[mt][e]);
+                const float up = fmaxf(m[mt], cross_group_max(top)), down = __builtin_amdgcn_exp2f((m[mt] - up) * a.scale);
+                m[mt] = up;
+                l[mt] *= down;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[mt][dt] *= down;
+                probabilities();
+            }
+            l[mt] += sum;
+            pf[mt][0] = __builtin_bit_cast(v8bf, v4i{pw[0], pw[1], pw[2], pw[3]});
+            pf[mt][1] = __builtin_bit_cast(v8bf, v4i{pw[4], pw[5], pw[6], pw[7]});
+        }
+        // ---- values
+        const float vsc = __int_as_float(v_scale << 23);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const v8bf v = decode8<E5M2>(vr[dt][2 * e], vr[dt][2 * e + 1], vsc);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) o[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[mt][e], o[mt][dt], 0, 0, 0);
+            }
+        load_v(next, page_v, more);
+    }
+    float* p = a.pieces + piece * (ROWS * (D + 2));
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const float sum = cross_group_sum(l[mt]);
+        const int rr = mt * 16 + col;
+        if (rr >= rows) continue;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *(v4f*)(p + rr * D + dt * 16 + grp * 4) = o[mt][dt];
+        if (grp == 0) {
+            p[ROWS * D + rr] = m[mt];
+            p[ROWS * D + ROWS + rr] = sum;
+        }
+    }
+}
+
+// What a step costs the chip's slot for a workgroup: 64 positions for 128 rows of a prefix; for one row tile of a sequence's own, of which a
+// workgroup does four side by side, and as much again for every tile.
+constexpr int COST_MANY = 3, COST_OWN = 2;
+constexpr int MIN_MANY = 2, MIN_OWN = 4;     // steps of a part
 
 // Rows of a sequence: tiles of 16 * MT.
 template <int D, bool E5M2, int MT, bool UNI>
 __global__ void __launch_bounds__(64 * WAVES, 2)
 cache_shared_kernel(SharedArgs x)
 {
-    using Few = FewLds<D, MT, WAVES>;
     using Many = ManyLds<D>;
-    constexpr size_t FEW = sizeof(typename Few::O) + sizeof(typename Few::Q) + sizeof(typename Few::Ml), MANY = sizeof(typename Many::K) + sizeof(typename Many::V);
-    __shared__ __attribute__((aligned(16))) char buffer[FEW > MANY ? FEW : MANY];
+    constexpr int ROWS = 16 * MT, MANY = sizeof(typename Many::K) + sizeof(typename Many::V), Q = MT > 1 ? MT * (D / 32) * 64 : 1;
+    static_assert(WAVES * Q * 16 <= MANY, "");
+    __shared__ __attribute__((aligned(16))) char buffer[MANY];
     __shared__ int odd[4], ends[4][WAVES], first[GROUPS_LDS + 1], steps[GROUPS_LDS];
     const CacheAttnArgs& a = x.a;
-    if (x.g.n <= GROUPS_LDS) {
+    const bool few_groups = x.g.n <= GROUPS_LDS;
+    if (few_groups) {
         for (int g = threadIdx.x; g <= x.g.n; g += 64 * WAVES) first[g] = x.g.first[g];
         for (int g = threadIdx.x; g < x.g.n; g += 64 * WAVES) steps[g] = shared_steps(x, x.g.shared[g]);
-        __syncthreads();
     }
-    const int lane = threadIdx.x & 63;
-    const Few few = {*(typename Few::O*)buffer, *(typename Few::Ml*)(buffer + sizeof(typename Few::O) + sizeof(typename Few::Q)), *(typename Few::Q*)(buffer + sizeof(typename Few::O))};
-    const OwnBehindPrefix own = {x, first, steps};
-
-    auto role = [&](int own_units, unsigned& block, unsigned& blocks) {
-        // ---- how much work the prefixes are
-        auto load = [&](int g, Bounds& r, int& tiles, int& visited) {
-            r = Bounds{0, 0, 0};
-            if (g < x.g.n) r = bounds_of(x, g);
-            tiles = (int)(((int64_t)(r.hi - r.lo) * x.rows_per_seq + ROWS_MANY - 1) / ROWS_MANY);
-            // under a window the steps differ from tile to tile: about as many as one token visits
-            visited = a.window ? min(r.steps, (int)min((int64_t)r.steps, (a.sinks + (int64_t)a.window + a.s.N) / STEP + 3)) : r.steps;
-        };
-        Bounds r;
-        int tiles, visited;
-        int64_t total = 0;
-        for (int base = 0; base < x.g.n; base += 64) {
-            load(base + lane, r, tiles, visited);
-            int64_t w = (int64_t)tiles * visited;
-            for (int s = 32; s; s >>= 1) w += __shfl_xor(w, s);
-            total += w;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // ---- all there is to do: steps of the sequences' own, 256 sequences at a time, ...
+    OwnSeq q4[4];
+    auto load4 = [&](int base, bool wait) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int b = base + 64 * k + lane;
+            const SeqInfo s = seq_of(a, min(b, a.s.B - 1));
+            q4[k].start = s.start;
+            q4[k].n = b < a.s.B ? s.n : 0;
         }
-        total *= a.c.Hkv;
-        // ---- which of the workgroups do which, by what the steps cost
-        const int64_t few_cost = ((int64_t)own_units << a.unit_shift) * COST_FEW, many_cost = total * COST_MANY;
-        int few_blocks = x.resident;
-        if (total) few_blocks = min(max((int)((double)x.resident * few_cost / (few_cost + many_cost)) / 8 * 8, 8), x.resident - 8);
-        block = blockIdx.x;
-        blocks = few_blocks;
-        if (total == 0 || (int)blockIdx.x < few_blocks) return (int)blockIdx.x < few_blocks;
-        // ---- pieces of the prefixes' items: equal parts of each
-        const int share = (int)max((total + (x.resident - few_blocks) - 1) / (x.resident - few_blocks), (int64_t)2);
-        auto pieces_of = [&] { return (int)min((int64_t)tiles * a.c.Hkv * ((visited + share - 1) / share), (int64_t)1 << 24); };
-        int all = 0;
-        for (int base = 0; base < x.g.n; base += 64) {
-            if (x.g.n > 64 || base > 0) load(base + lane, r, tiles, visited);
-            all += __builtin_amdgcn_readlane(wave_scan(pieces_of()), 63);
-            if (all < 0) return false;                              // (bounds that decrease)
+        if (wait) __syncthreads();                                // (the groups are in LDS)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int b = base + 64 * k + lane;
+            q4[k].own = 0;
+            if (base + 64 * k >= a.s.B) continue;                 // the same for all lanes
+            const int g = few_groups ? group_of([&](int i) { return first[i]; }, x.g.n, b) : group_of([&](int i) { return x.g.first[i]; }, x.g.n, b);
+            if (g >= 0) q4[k].own = few_groups ? steps[g] : shared_steps(x, x.g.shared[g]);
         }
-        // workgroups next to each other in the list on the same XCD: they read the same keys
-        const int per = (all + 7) / 8, p = blockIdx.x - few_blocks, at = p % 8 * per + p / 8;
-        if (p / 8 >= per || at >= all) return false;
+    };
+    auto tiles_of = [&](const OwnSeq& q) { return (int)(((unsigned)q.n * (unsigned)a.G + ROWS - 1) / ROWS); };
+    int64_t own_steps = 0, own_items = 0;
+    for (int base = 0; base < a.s.B; base += 256) {
+        load4(base, base == 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (base + 64 * k >= a.s.B) continue;
+            const int n = tiles_of(q4[k]);
+            own_items += n;
+            for (int i = 0; i < n; ++i) own_steps += own_range<ROWS>(a, q4[k], i).steps;
+        }
+    }
+    for (int s = 32; s; s >>= 1) {
+        own_steps += __shfl_xor(own_steps, s);
+        own_items += __shfl_xor(own_items, s);
+    }
+    own_steps = uniform(own_steps) * a.c.Hkv;
+    own_items = uniform(own_items) * a.c.Hkv;
+    // ... and of the groups' shared parts, 64 groups at a time
+    Bounds r;
+    int tiles, visited;
+    auto load = [&](int g) {
+        r = Bounds{0, 0, 0};
+        if (g < x.g.n) r = bounds_of(x, g);
+        tiles = (int)(((int64_t)(r.hi - r.lo) * x.rows_per_seq + ROWS_MANY - 1) / ROWS_MANY);
+        // under a window the steps differ from tile to tile: about as many as one token visits
+        visited = a.window ? min(r.steps, (int)min((int64_t)r.steps, (a.sinks + (int64_t)a.window + a.s.N) / STEP + 3)) : r.steps;
+    };
+    int64_t many_steps_all = 0;
+    for (int base = 0; base < x.g.n; base += 64) {
+        load(base + lane);
+        many_steps_all += (int64_t)tiles * visited;
+    }
+    for (int s = 32; s; s >>= 1) many_steps_all += __shfl_xor(many_steps_all, s);
+    many_steps_all = uniform(many_steps_all) * a.c.Hkv;
+    // ---- how many workgroups the items in several parts may take beyond one for each, by what the steps cost
+    const float many_cost = (float)many_steps_all * COST_MANY, own_cost = (float)(own_steps + own_items) * COST_OWN;
+    const int more_many = many_steps_all ? min(max(__builtin_amdgcn_readfirstlane((int)((float)x.more * many_cost / (many_cost + own_cost))), 1), x.more - 1) : 0;
+    const int more_own = x.more - more_many;
+    int share = MIN_MANY;
+    if (many_steps_all) share = (int)max((many_steps_all + more_many - 1) / more_many, (int64_t)MIN_MANY);
+    auto pieces_of = [&] { return (int)min((int64_t)tiles * a.c.Hkv * ((visited + share - 1) / share), (int64_t)1 << 24); };
+    int all = 0;
+    for (int base = 0; base < x.g.n; base += 64) {
+        if (x.g.n > 64) load(base + lane);
+        all += __builtin_amdgcn_readlane(wave_scan(pieces_of()), 63);
+        if (all < 0) return;                                      // (bounds that decrease)
+    }
+    const int per = (all + 7) / 8;
+    if ((int)blockIdx.x < 8 * per) {
+        // ---- a part of a prefix.  Workgroups next to each other in the list on the same XCD: they read the same keys
+        const int p = blockIdx.x, at = p % 8 * per + p / 8;
+        if (at >= all) return;
         int before = 0;
         for (int base = 0; base < x.g.n; base += 64) {
-            if (x.g.n > 64) load(base + lane, r, tiles, visited);
+            if (x.g.n > 64) load(base + lane);
             const int upto = wave_scan(pieces_of()), sum = __builtin_amdgcn_readlane(upto, 63);
-            if (at < before + sum) {
-                const int who = __builtin_ctzll(__ballot(before + upto > at));
-                Bounds mine;
-                mine.lo = __builtin_amdgcn_readlane(r.lo, who);
-                mine.hi = __builtin_amdgcn_readlane(r.hi, who);
-                mine.steps = __builtin_amdgcn_readlane(r.steps, who);
-                const int n_tiles = __builtin_amdgcn_readlane(tiles, who), parts = (__builtin_amdgcn_readlane(visited, who) + share - 1) / share;
-                const int first_piece = before + __builtin_amdgcn_readlane(upto, who) - n_tiles * a.c.Hkv * parts;
-                const int i = at - first_piece, tile = i % n_tiles, part = i / n_tiles % parts, h = i / n_tiles / parts;
-                const int item = h * n_tiles + tile;
-                const int64_t piece = (int64_t)first_piece + item * parts + part;
-                if (i < 0 || h >= a.c.Hkv || piece < 0 || piece >= x.max_pieces) return false;      // (bounds that decrease)
-                if (part == 0 && threadIdx.x == 0) x.split[(tiles_before(x, base + who, mine.lo)) * a.c.Hkv + item] = make_int2(first_piece + item * parts, parts);
-                const Many many = {*(typename Many::K*)buffer, *(typename Many::V*)(buffer + sizeof(typename Many::K)), odd};
-                prefix_part<D, E5M2, UNI>(x, many, ends, mine, h, tile, part, parts, piece);
-                return false;
+            if (at >= before + sum) {
+                before += sum;
+                continue;
             }
-            before += sum;
+            const int who = __builtin_ctzll(__ballot(before + upto > at));
+            Bounds mine;
+            mine.lo = __builtin_amdgcn_readlane(r.lo, who);
+            mine.hi = __builtin_amdgcn_readlane(r.hi, who);
+            mine.steps = __builtin_amdgcn_readlane(r.steps, who);
+            const int n_tiles = __builtin_amdgcn_readlane(tiles, who), parts = (__builtin_amdgcn_readlane(visited, who) + share - 1) / share;
+            const int first_piece = before + __builtin_amdgcn_readlane(upto, who) - n_tiles * a.c.Hkv * parts;
+            const int i = at - first_piece, tile = i % n_tiles, part = i / n_tiles % parts, h = i / n_tiles / parts;
+            const int item = h * n_tiles + tile;
+            const int64_t piece = (int64_t)first_piece + item * parts + part;
+            if (i < 0 || h >= a.c.Hkv || piece < 0 || piece >= x.max_pieces) return;      // (bounds that decrease)
+            if (part == 0 && threadIdx.x == 0) x.split[(tiles_before(x, base + who, mine.lo)) * a.c.Hkv + item] = make_int2(first_piece + item * parts, parts);
+            const Many many = {*(typename Many::K*)buffer, *(typename Many::V*)(buffer + sizeof(typename Many::K)), odd};
+            prefix_part<D, E5M2, UNI>(x, many, ends, mine, h, tile, part, parts, piece);
+            return;
         }
-        return false;
-    };
-    few_rows<D, E5M2, MT, WAVES, false, UNI>(a, few, own, role);
+        return;
+    }
+    // ---- a part of what a sequence has to itself: a wave by itself from here on
+    const int64_t unit64 = ((int64_t)blockIdx.x - 8 * per) * WAVES + wave;
+    const int len = (int)max((own_steps + 4 * (int64_t)more_own - 1) / (4 * (int64_t)more_own), (int64_t)MIN_OWN);
+    int64_t left = unit64;
+    OwnSeq sq = {0, 0, 0};
+    int b = -1, per_head = 0;
+    for (int base = 0; base < a.s.B && b < 0; base += 256) {
+        if (a.s.B > 256) load4(base, false);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (base + 64 * k >= a.s.B || b >= 0) continue;
+            const int n = tiles_of(q4[k]);
+            int units = 0;
+            for (int i = 0; i < n; ++i) units += max((own_range<ROWS>(a, q4[k], i).steps + len - 1) / len, 1);
+            const int upto = wave_scan(units);
+            const int64_t sum = (int64_t)__builtin_amdgcn_readlane(upto, 63) * a.c.Hkv;
+            if (left >= sum) {
+                left -= sum;
+                continue;
+            }
+            const int who = __builtin_ctzll(__ballot((int64_t)upto * a.c.Hkv > left));
+            b = base + 64 * k + who;
+            sq.start = __builtin_amdgcn_readlane(q4[k].start, who);
+            sq.n = __builtin_amdgcn_readlane(q4[k].n, who);
+            sq.own = __builtin_amdgcn_readlane(q4[k].own, who);
+            per_head = __builtin_amdgcn_readlane(units, who);
+            left -= (int64_t)(__builtin_amdgcn_readlane(upto, who) - per_head) * a.c.Hkv;
+        }
+    }
+    if (b < 0) return;
+    const int h = (int)left / per_head;
+    int part = (int)left - h * per_head, tile = 0, parts;
+    OwnRange range;
+    for (;; ++tile) {
+        range = own_range<ROWS>(a, sq, tile);
+        parts = max((range.steps + len - 1) / len, 1);
+        if (part < parts) break;
+        part -= parts;
+    }
+    if (part == 0 && lane == 0) a.split[((int64_t)b * a.c.Hkv + h) * a.row_tiles + tile] = make_int2((int)unit64, parts);
+    const int begin = (int)((int64_t)range.steps * part / parts), end = (int)((int64_t)range.steps * (part + 1) / parts);
+    own_part<D, E5M2, MT, UNI>(x, sq, range, b, h, tile, begin, end, unit64, (v8bf*)buffer + wave * Q);
 }
 
 // Joins the pieces of the prefix and of a sequence's own: a workgroup per sequence, kv head and 4 of its rows; threads over channels (4 each),
@@ -269,8 +600,9 @@ cache_shared_join_kernel(SharedArgs x)
     int own_first, own_n, many_first = 0, many_n = 0, many_row = 0;
     {
         const int2 sp = a.split[((int64_t)b * a.c.Hkv + h) * a.row_tiles + row / ROWS];
-        own_first = sp.x;
-        own_n = sp.y - sp.x + 1;
+        // (within the workspace whatever the bounds of the groups say, here and below)
+        own_first = max(sp.x, 0);
+        own_n = (int)min((int64_t)max(sp.y, 0), max(x.max_own - own_first, (int64_t)0));
     }
     if (g >= 0) {
         const Bounds r = bounds_of(x, g);
@@ -278,7 +610,6 @@ cache_shared_join_kernel(SharedArgs x)
             const int64_t in_group = (int64_t)(b - r.lo) * x.rows_per_seq + row;
             const int n_tiles = (int)(((int64_t)(r.hi - r.lo) * x.rows_per_seq + ROWS_MANY - 1) / ROWS_MANY);
             const int2 sp = x.split[tiles_before(x, g, r.lo) * a.c.Hkv + h * n_tiles + in_group / ROWS_MANY];
-            // (within the workspace whatever the bounds of the groups say)
             many_first = max(sp.x, 0);
             many_n = (int)min((int64_t)max(sp.y, 0), max(x.max_pieces - many_first, (int64_t)0));
             many_row = (int)(in_group % ROWS_MANY);
@@ -340,8 +671,8 @@ cache_shared_join_kernel(SharedArgs x)
 // ---------------------------------------------------------------------------------------------------------------- host
 // Sizes of a call: row tiles of a sequence, items of both kinds and their pieces at most.
 struct SharedSizes {
-    int mt, resident;
-    int64_t tiles, few_items, few_pieces, many_items, many_pieces, blocks;
+    int mt, more;
+    int64_t tiles, own_items, own_pieces, many_items, many_pieces, blocks;
     size_t bytes;
     bool fits;
 };
@@ -351,14 +682,14 @@ static SharedSizes sizes_of(const CacheView& c, int B, int G, int N, int n_group
     const int64_t rows = (int64_t)N * G;
     z.mt = rows <= 16 ? 1 : 2;
     z.tiles = (rows + 16 * z.mt - 1) / (16 * z.mt);
-    z.resident = (2 * cache_cus() + 15) / 16 * 16;
-    z.few_items = (int64_t)B * c.Hkv * z.tiles;
-    z.few_pieces = z.resident + z.few_items;
+    z.more = 2 * cache_cus();                     // as many as the chip holds
+    z.own_items = (int64_t)B * c.Hkv * z.tiles;
+    z.own_pieces = z.more * WAVES + z.own_items;
     z.many_items = ((int64_t)B * rows / ROWS_MANY + n_groups + 1) * c.Hkv;
-    z.many_pieces = z.resident + (B * rows / ROWS_MANY + std::min(n_groups, B) + 1) * (int64_t)c.Hkv;
-    z.blocks = z.resident + z.many_pieces;
-    z.bytes = (size_t)((z.few_pieces * 16 * z.mt + z.many_pieces * ROWS_MANY) * (c.D + 2) * 4 + (z.few_items + z.many_items) * 8);
-    z.fits = z.blocks * 256 <= 0xffffffffLL && (int64_t)B * c.Hkv * ((rows + 3) / 4) <= 0xffffffffLL / 512 && z.few_pieces < 1 << 30;
+    z.many_pieces = z.more + (B * rows / ROWS_MANY + std::min(n_groups, B) + 1) * (int64_t)c.Hkv;
+    z.blocks = z.many_pieces + (z.own_items + WAVES - 1) / WAVES + 16;
+    z.bytes = (size_t)((z.own_pieces * 16 * z.mt + z.many_pieces * ROWS_MANY) * (c.D + 2) * 4 + (z.own_items + z.many_items) * 8);
+    z.fits = z.blocks * 256 <= 0xffffffffLL && (int64_t)B * c.Hkv * ((rows + 3) / 4) <= 0xffffffffLL / 512;
     return z;
 }
 
@@ -392,22 +723,20 @@ int launch_cache_attn_shared(const CacheView& c, const Rows& q, const Rows& out,
     a.out = out;
     a.s = s;
     a.G = Hq / c.Hkv;
-    a.inv_g = (65536u + a.G - 1) / a.G;
     a.window = window;
     a.sinks = window ? sinks : 0;
     a.capacity = c.num_pages ? c.max_pages << c.page_shift : 0;
     a.scale = (float)(1.4426950408889634074 / sqrt((double)c.D));
     a.row_tiles = (int)z.tiles;
-    // the units of the line are counted in 31 bits
-    while (z.few_items * ((a.capacity / STEP >> a.unit_shift) + 2) > 0x7fffffff) ++a.unit_shift;
     x.g = groups;
     x.rows_per_seq = s.N * a.G;
-    x.resident = z.resident;
+    x.more = z.more;
     x.max_pieces = z.many_pieces;
+    x.max_own = z.own_pieces;
     a.pieces = (float*)workspace;
-    x.pieces = a.pieces + z.few_pieces * 16 * z.mt * (c.D + 2);
+    x.pieces = a.pieces + z.own_pieces * 16 * z.mt * (c.D + 2);
     a.split = (int2*)(x.pieces + z.many_pieces * ROWS_MANY * (c.D + 2));
-    x.split = a.split + z.few_items;
+    x.split = a.split + z.own_items;
     auto pick = [&](auto D, auto F) { return z.mt == 1 ? launch_shared<D, F != 0, 1>(x, z, stream) : launch_shared<D, F != 0, 2>(x, z, stream); };
     if (c.D == 128) return c.e5m2 ? pick(IC<128>{}, IC<1>{}) : pick(IC<128>{}, IC<0>{});
     return c.e5m2 ? pick(IC<64>{}, IC<1>{}) : pick(IC<64>{}, IC<0>{});
