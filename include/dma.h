@@ -294,7 +294,7 @@ size_t dma_cache_attn_workspace_bytes(const dma_kv_cache* cache, int B, int Hq, 
  *   length_i32  [B] int32, device, 4-byte aligned: positions that are kept, up to the table's width; below 1 none.  NULL: whole rows.
  *   So: beams in a new order (src = their origins), samples of one prompt (src = its row, length = its tokens), drafts taken back (src = b and
  *   a shorter length), sequences that end (src = -1).
- *   B > 16384: DMA_ERR_UNSUPPORTED.
+ *   B > 8192: DMA_ERR_UNSUPPORTED.
  */
 int dma_kv_fork(const dma_kv_cache* cache, void* refs_i32, int B, const void* src_i32, const void* length_i32, void* stream);
 

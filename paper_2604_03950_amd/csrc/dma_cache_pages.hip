@@ -10,17 +10,18 @@
 namespace dma {
 
 // ---------------------------------------------------------------------------------------------------------------- fork
-// A column of the new table depends on that column of the old one alone: a workgroup holds `cols` columns of all rows in LDS, so
-// that rows can take over each other's entries in place.
+// A column of the new table depends on that column of the old one alone: a workgroup holds some columns of all rows in LDS, so that rows can
+// take over each other's entries in place, and counts there how many rows take over each: what row r named is named (that - 1) times more.
+// One atomic at most per entry that is not taken over exactly once, instead of one for each that goes and one for each that comes.
 __global__ void __launch_bounds__(256)
 kv_fork_kernel(CacheView c, int* table, int* refs, int B, int cols_shift, const int* src, const int* length)
 {
-    extern __shared__ int tile[];
+    extern __shared__ int2 tile[];           // an entry, and how often it is taken over
     const int cols = 1 << cols_shift, n = B << cols_shift;
     for (int j0 = blockIdx.x << cols_shift; j0 < c.max_pages; j0 += gridDim.x << cols_shift) {
         for (int e = threadIdx.x; e < n; e += 256) {
             const int j = j0 + (e & (cols - 1));
-            tile[e] = j < c.max_pages ? table[(int64_t)(e >> cols_shift) * c.max_pages + j] : -1;
+            tile[e] = make_int2(j < c.max_pages ? table[(int64_t)(e >> cols_shift) * c.max_pages + j] : -1, 0);
         }
         __syncthreads();
         for (int e = threadIdx.x; e < n; e += 256) {
@@ -28,13 +29,21 @@ kv_fork_kernel(CacheView c, int* table, int* refs, int B, int cols_shift, const 
             if (j >= c.max_pages) continue;
             const int keep = length ? length[b] : 0x7fffffff;
             int page = -1;
-            if ((unsigned)from < (unsigned)B && (int64_t)j << c.page_shift < keep) page = tile[(from << cols_shift) + (e & (cols - 1))];
-            const int old = tile[e];
-            if ((unsigned)page >= c.page_limit) page = -1;
-            if (page == old) continue;
-            table[(int64_t)b * c.max_pages + j] = page;
-            if ((unsigned)old < c.page_limit) atomicAdd(&refs[old], -1);
-            if (page >= 0) atomicAdd(&refs[page], 1);
+            if ((unsigned)from < (unsigned)B && (int64_t)j << c.page_shift < keep) {
+                int2& taken = tile[(from << cols_shift) + (e & (cols - 1))];
+                page = taken.x;
+                if ((unsigned)page >= c.page_limit) page = -1;
+                else atomicAdd(&taken.y, 1);
+            }
+            if (page != tile[e].x) table[(int64_t)b * c.max_pages + j] = page;
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < n; e += 256) {
+            const int2 was = tile[e];
+            if (was.y == 1 || (unsigned)was.x >= c.page_limit) continue;
+            // A count of one is this entry's own: every other one that named the page has been taken off it, and nobody else changes it.
+            if (refs[was.x] == 1) refs[was.x] = was.y;
+            else atomicAdd(&refs[was.x], was.y - 1);
         }
         __syncthreads();
     }
@@ -44,26 +53,41 @@ int launch_kv_fork(const CacheView& c, int* refs, int B, const int* src, const i
 {
     if (c.max_pages == 0) return DMA_OK_;
     int shift = 4;
-    while (shift && (B << shift) > 16384) --shift;                      // 64 KiB of LDS
+    while (shift && (B << shift) > FORK_ROWS_MAX) --shift;              // 64 KiB of LDS
+    // ... and fewer columns where that leaves CUs without any
+    while (shift > 2 && (c.max_pages >> shift) < 512) --shift;
     const int blocks = std::min((c.max_pages + (1 << shift) - 1) >> shift, 4096);
-    return launch_lds(kv_fork_kernel, dim3(blocks), dim3(256), (size_t)(B << shift) * 4, stream, c, (int*)c.page_table, refs, B, shift, src, length);
+    return launch_lds(kv_fork_kernel, dim3(blocks), dim3(256), (size_t)(B << shift) * 8, stream, c, (int*)c.page_table, refs, B, shift, src, length);
 }
 
 // --------------------------------------------------------------------------------------------------------- page copies
-// A slice of a page's codes, by a workgroup of 256 threads: 16 bytes per thread and turn, four in flight.
-DMA_DEV void copy_slice(const uint8_t* src, uint8_t* dst, int64_t from, int64_t to)
+// A slice of a page's codes (the keys' slices, then the values', each side `bytes`) from page `from` to page `to`, by a workgroup of 256 threads:
+// 16 bytes per thread and turn, four in flight.  Stores pass the caches by, which hold less than what is copied; loads as well where each page is
+// read once (ONCE; where samples of one prompt part, all of them copy one page).  1000 pages of 131 KB: both 45 us = 5.8 TB/s, stores alone 46.4,
+// neither 51.6.
+constexpr int SLICE = 16384;
+template <bool ONCE>
+DMA_DEV void copy_slice(const CacheView& c, int64_t bytes, int from, int to, int slice)
 {
-    for (int64_t at = from + threadIdx.x * 16; at < to; at += 4 * 256 * 16) {
-        v4i w[4];
+    const int side = (int)((bytes + SLICE - 1) / SLICE);
+    const uint8_t* codes = slice < side ? c.k_codes : c.v_codes;
+    const int64_t first = (int64_t)(slice < side ? slice : slice - side) * SLICE, end = min(first + SLICE, bytes);
+    const uint8_t* src = codes + from * bytes;
+    uint8_t* dst = (uint8_t*)codes + to * bytes;
+    v4i w[4];
+    if (end - first == SLICE) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (at + u * 4096 < to) w[u] = __builtin_nontemporal_load((const v4i*)(src + at + u * 4096));
+        for (int u = 0; u < 4; ++u) {
+            const v4i* at = (const v4i*)(src + first + threadIdx.x * 16 + u * 4096);
+            w[u] = ONCE ? __builtin_nontemporal_load(at) : *at;
+        }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (at + u * 4096 < to) __builtin_nontemporal_store(w[u], (v4i*)(dst + at + u * 4096));
+        for (int u = 0; u < 4; ++u) __builtin_nontemporal_store(w[u], (v4i*)(dst + first + threadIdx.x * 16 + u * 4096));
+    } else {
+        for (int64_t at = first + threadIdx.x * 16; at < end; at += 4096) *(v4i*)(dst + at) = *(const v4i*)(src + at);
     }
 }
-constexpr int SLICE = 16384;
+DMA_DEV_CONSTEXPR int64_t slices_of(int64_t bytes) { return 2 * ((bytes + SLICE - 1) / SLICE); }
 
 // Where thread t of 1024 stands among those before it: the sum of `mine` over them, and over all in `total`.
 DMA_DEV int scan_1024(int mine, int* wave_sums, int& total)
@@ -160,37 +184,35 @@ kv_reserve_kernel(CacheView c, int* table, int* refs, Spans s, int pages_per_seq
 }
 
 // What became of the entries: shared pages are one holder poorer, the earlier tokens in them are copied, other new pages hold nothing.
-// blockIdx.y: a slice of the copies.
+// blockIdx.y: a slice of the copies; the first has the rest as well.
 __global__ void __launch_bounds__(256)
 kv_part_kernel(CacheView c, const int* table, int* refs, Spans s, int pages_per_seq, const int* left)
 {
     const int64_t bytes = (int64_t)c.Hkv * c.D << c.page_shift;
     for (int b = blockIdx.x; b < s.B; b += gridDim.x) {
-        const int start = s.start[b];
+        const int start = s.start[b], j0 = start >> c.page_shift;
         const int* l = left + (int64_t)b * pages_per_seq;
         const int* row = table + (int64_t)b * c.max_pages;
-        const int j0 = start >> c.page_shift;
         const bool part = start >= 0 && (start & ((1 << c.page_shift) - 1)) != 0;
-        if (blockIdx.y == 0)
-            for (int k = threadIdx.x; k < pages_per_seq; k += 256) {
+        if (blockIdx.y == 0) {
+            // entries times kv heads over the threads
+            const int step = max(256 / c.Hkv, 1), k0 = threadIdx.x / c.Hkv, h0 = c.Hkv > 256 ? threadIdx.x : threadIdx.x - k0 * c.Hkv;
+            for (int k = c.Hkv > 256 ? 0 : k0; k < pages_per_seq && (c.Hkv > 256 || k0 < step); k += step) {
                 const int old = l[k];
                 if (old == NOT_GIVEN) continue;
-                if (old >= 0) atomicAdd(&refs[old], -1);
+                if (old >= 0 && h0 == 0) atomicAdd(&refs[old], -1);
                 const bool copied = old >= 0 && k == 0 && part;
                 const int64_t to = (int64_t)row[j0 + k] * c.Hkv, from = copied ? (int64_t)old * c.Hkv : 0;
-                for (int h = 0; h < c.Hkv; ++h) {
+                for (int h = h0; h < c.Hkv; h += 256) {
                     c.k_scales[to + h] = copied ? c.k_scales[from + h] : 255;
                     c.v_scales[to + h] = copied ? c.v_scales[from + h] : 255;
                 }
             }
+        }
         const int old = l[0];
         if (old < 0 || !part) continue;
-        const int64_t to = row[j0] * bytes, from = old * bytes;
-        for (int64_t at = (int64_t)blockIdx.y * SLICE; at < 2 * bytes; at += (int64_t)gridDim.y * SLICE) {
-            // slices of the keys, then of the values; one may hold the end of the keys and the start of the values
-            if (at < bytes) copy_slice(c.k_codes + from, c.k_codes + to, at, min(at + SLICE, bytes));
-            if (at + SLICE > bytes) copy_slice(c.v_codes + from, c.v_codes + to, max(at - bytes, (int64_t)0), min(at + SLICE - bytes, bytes));
-        }
+        const int to = row[j0];
+        for (int64_t slice = blockIdx.y; slice < slices_of(bytes); slice += gridDim.y) copy_slice<false>(c, bytes, old, to, (int)slice);
     }
 }
 
@@ -201,7 +223,7 @@ int launch_kv_reserve(const CacheView& c, int* refs, const Spans& s, int* missin
     const int pages = (int)reserve_pages(c, s.N);
     const int rc = launch(kv_reserve_kernel, dim3(1), dim3(1024), stream, c, (int*)c.page_table, refs, s, pages, missing, workspace);
     if (rc != DMA_OK_ || pages == 0) return rc;
-    const int64_t slices = std::min<int64_t>(((2LL * c.Hkv * c.D << c.page_shift) + SLICE - 1) / SLICE, 64);
+    const int64_t slices = std::min<int64_t>(slices_of((int64_t)c.Hkv * c.D << c.page_shift), 64);
     return launch(kv_part_kernel, dim3(std::min(s.B, 8192), (unsigned)slices), dim3(256), stream, c, c.page_table, refs, s, pages, (const int*)workspace);
 }
 
@@ -262,13 +284,12 @@ __global__ void __launch_bounds__(256)
 kv_compact_kernel(CacheView c, int* table, int* refs, int64_t entries, const int* moved, const Moves* moves)
 {
     const int count = moves->count;
-    const int64_t bytes = (int64_t)c.Hkv * c.D << c.page_shift, slices = (bytes + SLICE - 1) / SLICE, all = 2 * slices * count;
+    const int64_t bytes = (int64_t)c.Hkv * c.D << c.page_shift, slices = slices_of(bytes), all = slices * count;
     for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
-        const int64_t which = i / (2 * slices), part = i % (2 * slices), at = part % slices * SLICE;
+        const int64_t which = i / slices;
+        const int part = (int)(i - which * slices);
         const int2 m = moves->move[which];
-        const int64_t from = m.x * bytes, to = m.y * bytes;
-        if (part < slices) copy_slice(c.k_codes + from, c.k_codes + to, at, min(at + SLICE, bytes));
-        else copy_slice(c.v_codes + from, c.v_codes + to, at, min(at + SLICE, bytes));
+        copy_slice<true>(c, bytes, m.x, m.y, part);
         if (part == 0) {
             for (int h = threadIdx.x; h < c.Hkv; h += 256) {
                 c.k_scales[(int64_t)m.y * c.Hkv + h] = c.k_scales[(int64_t)m.x * c.Hkv + h];
@@ -291,7 +312,9 @@ int launch_kv_compact(const CacheView& c, int* refs, int B, int* used, int* move
 {
     const int rc = launch(kv_compact_plan_kernel, dim3(1), dim3(1024), stream, c, (const int*)refs, used, moved, (Moves*)workspace);
     if (rc != DMA_OK_) return rc;
-    return launch(kv_compact_kernel, dim3(2048), dim3(256), stream, c, (int*)c.page_table, refs, (int64_t)B * c.max_pages, (const int*)moved, (const Moves*)workspace);
+    // a slice for each workgroup, as far as the host knows how many there can be
+    const int64_t slices = c.num_pages / 2 * slices_of((int64_t)c.Hkv * c.D << c.page_shift), blocks = std::min<int64_t>(std::max<int64_t>(slices, 1024), 16384);
+    return launch(kv_compact_kernel, dim3((unsigned)blocks), dim3(256), stream, c, (int*)c.page_table, refs, (int64_t)B * c.max_pages, (const int*)moved, (const Moves*)workspace);
 }
 
 }  // namespace dma

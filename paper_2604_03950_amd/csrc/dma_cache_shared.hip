@@ -20,10 +20,13 @@ struct SharedArgs {
     CacheAttnArgs a;         // pieces and split (first piece, how many): of what the sequences have to themselves, per tile of 16 * MT rows
     Groups g;
     int rows_per_seq;        // query rows of a kv head and sequence: N * G
+    int piece_rows;          // of a sequence's own piece: at most 16 * MT
+    int piece_size;          // in floats: sums, then maxima and weights, up to a multiple of 4
     float* pieces;           // of the prefixes: per workgroup [128][D] sums, [128] maxima, [128] weights
     int2* split;             // per kv head and row tile: the first piece and how many
     int64_t max_pieces, max_own;
-    int more;                // workgroups beyond one for each row tile of a prefix and for four tiles of the sequences: items in several parts
+    int cus;
+    int more_own;            // waves beyond one for each row tile of the sequences: tiles in several parts
 };
 
 struct Bounds {
@@ -65,12 +68,13 @@ struct OwnRange {
     int own, sink_steps, first, steps;
     DMA_DEV int position(int j) const { return (j < sink_steps ? own + j : first + j - sink_steps) * STEP; }
 };
-template <int ROWS>
+// (A start behind the table is brought to its end: what that lets in too much is not seen by any row.)
+template <int ROWS, bool ONE>
 DMA_DEV OwnRange own_range(const CacheAttnArgs& a, const OwnSeq& q, int tile)
 {
-    const int64_t from = (int64_t)q.start + tile * ROWS / a.G, to = (int64_t)q.start + min(q.n - 1, (tile * ROWS + ROWS - 1) / a.G);
-    const int hi = (int)min(to + 1, (int64_t)a.capacity);
-    const int lo = a.window ? (int)min(max(from - a.window + 1, (int64_t)0), (int64_t)hi) : 0;
+    const int start = min(q.start, a.capacity), from = start + (ONE ? 0 : token_of<true>(a, tile * ROWS));
+    const int hi = min(start + 1 + (ONE ? q.n - 1 : min(q.n - 1, token_of<true>(a, tile * ROWS + ROWS - 1))), a.capacity);
+    const int lo = a.window ? min(max(from - a.window + 1, 0), hi) : 0;
     OwnRange r;
     r.own = q.own;
     r.first = max(lo / STEP, q.own);
@@ -83,12 +87,6 @@ DMA_DEV OwnRange own_range(const CacheAttnArgs& a, const OwnSeq& q, int tile)
     return r;
 }
 
-// The same in all lanes, and known to be: what is derived from it takes scalar loads and branches.
-DMA_DEV int64_t uniform(int64_t x)
-{
-    return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
-}
-
 DMA_DEV int wave_scan(int x)                 // the sum up to and with this lane's
 {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);       // row_shr:1, 2, 4, 8
@@ -99,10 +97,33 @@ DMA_DEV int wave_scan(int x)                 // the sum up to and with this lane
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
+DMA_DEV int wave_max(int x)
+{
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+// The sum over the lanes.  In binary32: how work is divided needs no more, and every wave adds in the same order.
+DMA_DEV float wave_sum(float v)
+{
+#define DMA_SHIFTED(ctrl, rows) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, false))
+    v += DMA_SHIFTED(0x111, 0xf);
+    v += DMA_SHIFTED(0x112, 0xf);
+    v += DMA_SHIFTED(0x114, 0xf);
+    v += DMA_SHIFTED(0x118, 0xf);
+    v += DMA_SHIFTED(0x142, 0xa);
+    v += DMA_SHIFTED(0x143, 0xc);
+#undef DMA_SHIFTED
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
 
 // One workgroup's part of the prefixes: 128 rows of a group, some of their steps, into piece `piece`.
 template <int D, bool E5M2, bool UNI>
-DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)[4][WAVES], const Bounds& g, int h, int tile, int part, int parts, int64_t piece)
+DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)[4][WAVES], const Bounds& g, int h, int tile, int part, int parts, float early, bool late, int64_t piece)
 {
     const CacheAttnArgs& a = x.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
@@ -111,7 +132,7 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     // ---- this lane's row: sequence, token and head
     const int64_t r = min((int64_t)tile * ROWS_MANY + wave * 32 + col, all_rows - 1);
     const int b = g.lo + (int)((unsigned)r / (unsigned)x.rows_per_seq), in_seq = (int)((unsigned)r % (unsigned)x.rows_per_seq);
-    const int tok = in_seq / a.G;
+    const int tok = token_of<true>(a, in_seq);
     v8bf qf[D / 16];
     {
         const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + in_seq - tok * a.G) * a.q.stride_head + tok * a.q.stride_token;
@@ -126,10 +147,6 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     view.my_rows = my_rows;
     view.vis_hi = exists ? cut_position(at) : -1;
     view.vis_lo = exists && a.window ? cut_position(at - a.window + 1) : 0;
-    auto wave_max = [](int v) {
-        for (int s = 16; s; s >>= 1) v = max(v, __shfl_xor(v, s));
-        return __builtin_amdgcn_readfirstlane(v);
-    };
     view.all_hi = -wave_max(exists ? -view.vis_hi : -POS_MAX);
     view.some_hi = wave_max(view.vis_hi);
     view.all_lo = wave_max(view.vis_lo);
@@ -156,7 +173,9 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     range.sink_steps = (min(a.sinks, hi) + STEP - 1) / STEP;
     if (range.sink_steps >= range.first) range.sink_steps = range.first = 0;
     range.steps = range.sink_steps + (hi + STEP - 1) / STEP - range.first;
-    const int begin = (int)((int64_t)range.steps * part / parts), end = (int)((int64_t)range.steps * (part + 1) / parts);
+    int begin = (int)((int64_t)range.steps * part / parts), end = (int)((int64_t)range.steps * (part + 1) / parts);
+    const int cut = min(begin + __builtin_amdgcn_readfirstlane((int)ceilf((float)(end - begin) * early)), end);
+    (late ? begin : end) = cut;
     v16f o[D / 32];
     float m, l;
     many_steps<D, E5M2, WAVES, UNI>(a, lds, g.lo, h, range, begin, end, view, qf, o, m, l);
@@ -237,7 +256,7 @@ DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& ran
     const int64_t from = sq.start;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = r / a.G;
+        const int r = min(mt * 16 + col, rows - 1) + tile * ROWS, i = token_of<true>(a, r);
         const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + r - i * a.G) * a.q.stride_head + i * a.q.stride_token;
 #pragma unroll
         for (int ks = 0; ks < 2 * KJ; ++ks) qf[mt][ks] = *(const v8bf*)(qp + ((ks >> 1) * 64 + grp * 16 + (ks & 1) * 8) * 2);
@@ -245,7 +264,7 @@ DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& ran
         vis_lo[mt] = a.window ? cut_position(from + i - a.window + 1) : 0;
     }
     // ... and what all of them see
-    const int all_hi = cut_position(from + tile * ROWS / a.G), all_lo = a.window ? cut_position(from + (tile * ROWS + rows - 1) / a.G - a.window + 1) : 0;
+    const int all_hi = cut_position(from + token_of<true>(a, tile * ROWS)), all_lo = a.window ? cut_position(from + token_of<true>(a, tile * ROWS + rows - 1) - a.window + 1) : 0;
     __builtin_amdgcn_sched_barrier(0);
     if (begin < end) {
         const int page_v = there(pv, begin, grp);
@@ -402,7 +421,7 @@ DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& ran
             }
         load_v(next, page_v, more);
     }
-    float* p = a.pieces + piece * (ROWS * (D + 2));
+    float* p = a.pieces + piece * x.piece_size;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         const float sum = cross_group_sum(l[mt]);
@@ -411,16 +430,18 @@ DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& ran
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) *(v4f*)(p + rr * D + dt * 16 + grp * 4) = o[mt][dt];
         if (grp == 0) {
-            p[ROWS * D + rr] = m[mt];
-            p[ROWS * D + ROWS + rr] = sum;
+            p[x.piece_rows * D + rr] = m[mt];
+            p[x.piece_rows * D + x.piece_rows + rr] = sum;
         }
     }
 }
 
-// What a step costs the chip's slot for a workgroup: 64 positions for 128 rows of a prefix; for one row tile of a sequence's own, of which a
-// workgroup does four side by side, and as much again for every tile.
-constexpr int COST_MANY = 3, COST_OWN = 2;
-constexpr int MIN_MANY = 2, MIN_OWN = 4;     // steps of a part
+constexpr int MIN_MANY = 2, MIN_OWN = 4;     // steps of a part at least
+// What the sequences' own parts take of a CU's time beside a prefix's part, in steps of that: to begin with, and per step.
+constexpr float OWN_FIRST = 4.5f, OWN_STEP = 0.9f;
+// Of the steps that two parts of prefixes do side by side on a CU, those of the one that began later (the SIMDs prefer older waves).
+constexpr float LATE = 0.42f;
+constexpr float MIN_LATE = 3.f;              // steps of a late part at least
 
 // Rows of a sequence: tiles of 16 * MT.
 template <int D, bool E5M2, int MT, bool UNI>
@@ -459,127 +480,165 @@ cache_shared_kernel(SharedArgs x)
             if (g >= 0) q4[k].own = few_groups ? steps[g] : shared_steps(x, x.g.shared[g]);
         }
     };
-    auto tiles_of = [&](const OwnSeq& q) { return (int)(((unsigned)q.n * (unsigned)a.G + ROWS - 1) / ROWS); };
-    int64_t own_steps = 0, own_items = 0;
+    constexpr bool ONE = MT == 1;                                 // a sequence's rows are one tile
+    auto tiles_of = [&](const OwnSeq& q) { return ONE ? q.n > 0 : (int)(((unsigned)q.n * (unsigned)a.G + ROWS - 1) / ROWS); };
+    float own_steps = 0.f;
     for (int base = 0; base < a.s.B; base += 256) {
         load4(base, base == 0);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (base + 64 * k >= a.s.B) continue;
             const int n = tiles_of(q4[k]);
-            own_items += n;
-            for (int i = 0; i < n; ++i) own_steps += own_range<ROWS>(a, q4[k], i).steps;
+            for (int i = 0; i < n; ++i) own_steps += (float)own_range<ROWS, ONE>(a, q4[k], i).steps;
         }
     }
-    for (int s = 32; s; s >>= 1) {
-        own_steps += __shfl_xor(own_steps, s);
-        own_items += __shfl_xor(own_items, s);
-    }
-    own_steps = uniform(own_steps) * a.c.Hkv;
-    own_items = uniform(own_items) * a.c.Hkv;
+    own_steps = wave_sum(own_steps) * a.c.Hkv;
     // ... and of the groups' shared parts, 64 groups at a time
     Bounds r;
     int tiles, visited;
     auto load = [&](int g) {
         r = Bounds{0, 0, 0};
-        if (g < x.g.n) r = bounds_of(x, g);
-        tiles = (int)(((int64_t)(r.hi - r.lo) * x.rows_per_seq + ROWS_MANY - 1) / ROWS_MANY);
+        if (g < x.g.n) {
+            r.lo = min(max(few_groups ? first[g] : x.g.first[g], 0), a.s.B);
+            r.hi = min(max(few_groups ? first[g + 1] : x.g.first[g + 1], r.lo), a.s.B);
+            r.steps = few_groups ? steps[g] : shared_steps(x, x.g.shared[g]);
+        }
+        tiles = (int)(((unsigned)(r.hi - r.lo) * (unsigned)x.rows_per_seq + ROWS_MANY - 1) / ROWS_MANY);
         // under a window the steps differ from tile to tile: about as many as one token visits
-        visited = a.window ? min(r.steps, (int)min((int64_t)r.steps, (a.sinks + (int64_t)a.window + a.s.N) / STEP + 3)) : r.steps;
+        visited = a.window ? (int)min((int64_t)r.steps, (a.sinks + (int64_t)a.window + a.s.N) / STEP + 3) : r.steps;
     };
-    int64_t many_steps_all = 0;
+    float many = 0.f;
     for (int base = 0; base < x.g.n; base += 64) {
         load(base + lane);
-        many_steps_all += (int64_t)tiles * visited;
+        many += (float)tiles * (float)visited;
     }
-    for (int s = 32; s; s >>= 1) many_steps_all += __shfl_xor(many_steps_all, s);
-    many_steps_all = uniform(many_steps_all) * a.c.Hkv;
-    // ---- how many workgroups the items in several parts may take beyond one for each, by what the steps cost
-    const float many_cost = (float)many_steps_all * COST_MANY, own_cost = (float)(own_steps + own_items) * COST_OWN;
-    const int more_many = many_steps_all ? min(max(__builtin_amdgcn_readfirstlane((int)((float)x.more * many_cost / (many_cost + own_cost))), 1), x.more - 1) : 0;
-    const int more_own = x.more - more_many;
-    int share = MIN_MANY;
-    if (many_steps_all) share = (int)max((many_steps_all + more_many - 1) / more_many, (int64_t)MIN_MANY);
+    many = wave_sum(many) * a.c.Hkv;
+    // ---- steps of a part
+    auto part_of = [](float all, int parts, int least) {
+        const float s = fminf(all / (float)parts, 1e9f);
+        return max(__builtin_amdgcn_readfirstlane((int)ceilf(s)), least);
+    };
+    int share = part_of(many, x.cus, MIN_MANY);
+    const int len = part_of(own_steps, x.more_own, MIN_OWN);
     auto pieces_of = [&] { return (int)min((int64_t)tiles * a.c.Hkv * ((visited + share - 1) / share), (int64_t)1 << 24); };
-    int all = 0;
-    for (int base = 0; base < x.g.n; base += 64) {
-        if (x.g.n > 64) load(base + lane);
-        all += __builtin_amdgcn_readlane(wave_scan(pieces_of()), 63);
-        if (all < 0) return;                                      // (bounds that decrease)
-    }
-    const int per = (all + 7) / 8;
-    if ((int)blockIdx.x < 8 * per) {
-        // ---- a part of a prefix.  Workgroups next to each other in the list on the same XCD: they read the same keys
-        const int p = blockIdx.x, at = p % 8 * per + p / 8;
-        if (at >= all) return;
-        int before = 0;
+    auto count = [&] {
+        int all = 0;
         for (int base = 0; base < x.g.n; base += 64) {
             if (x.g.n > 64) load(base + lane);
-            const int upto = wave_scan(pieces_of()), sum = __builtin_amdgcn_readlane(upto, 63);
-            if (at >= before + sum) {
-                before += sum;
-                continue;
+            all = max(all, 0) + __builtin_amdgcn_readlane(wave_scan(pieces_of()), 63);
+        }
+        return all;
+    };
+    int all = count();
+    if (all > x.cus && all < 2 * x.cus) {                         // a few more than there are CUs: longer ones instead
+        share = (int)((int64_t)share * all / x.cus) + 1;
+        all = count();
+    }
+    // A CU holds two workgroups.  A part of the prefixes for each goes first, and the sequences' own parts pass through the other place; behind them
+    // that place takes what is left of each part, so much that both end together.
+    const float each = many / (float)max(all, 1), own_time = OWN_FIRST + OWN_STEP * own_steps / (float)x.cus;
+    float early = 1.f;
+    if (LATE * (each - own_time) > MIN_LATE) early = 1.f - LATE * (1.f - own_time / each);
+    const bool two = early < 1.f;
+    const int per = (all + 7) / 8;
+    // ---- who does what, in the order of the workgroups
+    int p = blockIdx.x;
+    const bool late = p >= 8 * per;
+    if (late) {
+        // parts of what the sequences have to themselves, for each wave of its own: unit after unit in equal steps through all of them
+        int units[4], upto[4], all_units = 0;
+        auto count4 = [&](int base) {
+            int sum = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                units[k] = upto[k] = 0;
+                if (base + 64 * k >= a.s.B) continue;
+                const int n = tiles_of(q4[k]);
+                for (int i = 0; i < n; ++i) units[k] += max((own_range<ROWS, ONE>(a, q4[k], i).steps + len - 1) / len, 1);
+                upto[k] = wave_scan(units[k]);
+                sum += __builtin_amdgcn_readlane(upto[k], 63);
             }
-            const int who = __builtin_ctzll(__ballot(before + upto > at));
-            Bounds mine;
-            mine.lo = __builtin_amdgcn_readlane(r.lo, who);
-            mine.hi = __builtin_amdgcn_readlane(r.hi, who);
-            mine.steps = __builtin_amdgcn_readlane(r.steps, who);
-            const int n_tiles = __builtin_amdgcn_readlane(tiles, who), parts = (__builtin_amdgcn_readlane(visited, who) + share - 1) / share;
-            const int first_piece = before + __builtin_amdgcn_readlane(upto, who) - n_tiles * a.c.Hkv * parts;
-            const int i = at - first_piece, tile = i % n_tiles, part = i / n_tiles % parts, h = i / n_tiles / parts;
-            const int item = h * n_tiles + tile;
-            const int64_t piece = (int64_t)first_piece + item * parts + part;
-            if (i < 0 || h >= a.c.Hkv || piece < 0 || piece >= x.max_pieces) return;      // (bounds that decrease)
-            if (part == 0 && threadIdx.x == 0) x.split[(tiles_before(x, base + who, mine.lo)) * a.c.Hkv + item] = make_int2(first_piece + item * parts, parts);
-            const Many many = {*(typename Many::K*)buffer, *(typename Many::V*)(buffer + sizeof(typename Many::K)), odd};
-            prefix_part<D, E5M2, UNI>(x, many, ends, mine, h, tile, part, parts, piece);
+            return sum * a.c.Hkv;
+        };
+        for (int base = 0; base < a.s.B; base += 256) {
+            if (a.s.B > 256) load4(base, false);
+            all_units += count4(base);
+        }
+        all_units = min(all_units, x.max_own);
+        const int own_blocks = min((all_units + WAVES - 1) / WAVES, max(2 * x.cus - 8 * per, x.cus));
+        p -= 8 * per;
+        if (p < own_blocks) {
+            for (int unit = p * WAVES + wave; unit < all_units; unit += own_blocks * WAVES) {
+                int left = unit, b = -1, per_head = 1;
+                OwnSeq sq = {0, 0, 0};
+                for (int base = 0; base < a.s.B && b < 0; base += 256) {
+                    if (a.s.B > 256) {
+                        load4(base, false);
+                        count4(base);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (base + 64 * k >= a.s.B || b >= 0) continue;
+                        const int sum = __builtin_amdgcn_readlane(upto[k], 63) * a.c.Hkv;
+                        if (left >= sum) {
+                            left -= sum;
+                            continue;
+                        }
+                        const int who = __builtin_ctzll(__ballot(upto[k] * a.c.Hkv > left));
+                        b = base + 64 * k + who;
+                        sq.start = __builtin_amdgcn_readlane(q4[k].start, who);
+                        sq.n = __builtin_amdgcn_readlane(q4[k].n, who);
+                        sq.own = __builtin_amdgcn_readlane(q4[k].own, who);
+                        per_head = __builtin_amdgcn_readlane(units[k], who);
+                        left -= (__builtin_amdgcn_readlane(upto[k], who) - per_head) * a.c.Hkv;
+                    }
+                }
+                if (b < 0) return;
+                const int h = left / per_head;
+                int part = left - h * per_head, tile = 0, parts;
+                OwnRange range;
+                for (;; ++tile) {
+                    range = own_range<ROWS, ONE>(a, sq, tile);
+                    parts = max((range.steps + len - 1) / len, 1);
+                    if (ONE || part < parts) break;
+                    part -= parts;
+                }
+                if (part == 0 && lane == 0) a.split[((int64_t)b * a.c.Hkv + h) * a.row_tiles + tile] = make_int2(unit, parts);
+                const int begin = (int)((int64_t)range.steps * part / parts), end = (int)((int64_t)range.steps * (part + 1) / parts);
+                own_part<D, E5M2, MT, UNI>(x, sq, range, b, h, tile, begin, end, unit, (v8bf*)buffer + wave * Q);
+            }
             return;
         }
+        if (!two) return;
+        p -= own_blocks;
+    }
+    // a part of a prefix.  Workgroups next to each other in the list on the same XCD: they read the same keys
+    const int at = p % 8 * per + p / 8;
+    if (p >= 8 * per || at >= all) return;
+    int before = 0;
+    for (int base = 0; base < x.g.n; base += 64) {
+        if (x.g.n > 64) load(base + lane);
+        const int upto = wave_scan(pieces_of()), sum = __builtin_amdgcn_readlane(upto, 63);
+        if (at >= before + sum) {
+            before += sum;
+            continue;
+        }
+        const int who = __builtin_ctzll(__ballot(before + upto > at));
+        Bounds mine;
+        mine.lo = __builtin_amdgcn_readlane(r.lo, who);
+        mine.hi = __builtin_amdgcn_readlane(r.hi, who);
+        mine.steps = __builtin_amdgcn_readlane(r.steps, who);
+        const int n_tiles = __builtin_amdgcn_readlane(tiles, who), parts = (__builtin_amdgcn_readlane(visited, who) + share - 1) / share;
+        const int first_piece = before + __builtin_amdgcn_readlane(upto, who) - n_tiles * a.c.Hkv * parts;
+        const int i = at - first_piece, rest = i / n_tiles, tile = i - rest * n_tiles, h = rest / parts, part = rest - h * parts;
+        const int item = h * n_tiles + tile;
+        const int64_t piece = two ? 2 * ((int64_t)first_piece + item * parts + part) + late : (int64_t)first_piece + item * parts + part;
+        if (i < 0 || h >= a.c.Hkv || piece < 0 || piece >= x.max_pieces) return;          // (bounds that decrease)
+        if (part == 0 && !late && threadIdx.x == 0) x.split[(tiles_before(x, base + who, mine.lo)) * a.c.Hkv + item] = make_int2((first_piece + item * parts) << two, parts << two);
+        const Many lds = {*(typename Many::K*)buffer, *(typename Many::V*)(buffer + sizeof(typename Many::K)), odd};
+        prefix_part<D, E5M2, UNI>(x, lds, ends, mine, h, tile, part, parts, early, late, piece);
         return;
     }
-    // ---- a part of what a sequence has to itself: a wave by itself from here on
-    const int64_t unit64 = ((int64_t)blockIdx.x - 8 * per) * WAVES + wave;
-    const int len = (int)max((own_steps + 4 * (int64_t)more_own - 1) / (4 * (int64_t)more_own), (int64_t)MIN_OWN);
-    int64_t left = unit64;
-    OwnSeq sq = {0, 0, 0};
-    int b = -1, per_head = 0;
-    for (int base = 0; base < a.s.B && b < 0; base += 256) {
-        if (a.s.B > 256) load4(base, false);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (base + 64 * k >= a.s.B || b >= 0) continue;
-            const int n = tiles_of(q4[k]);
-            int units = 0;
-            for (int i = 0; i < n; ++i) units += max((own_range<ROWS>(a, q4[k], i).steps + len - 1) / len, 1);
-            const int upto = wave_scan(units);
-            const int64_t sum = (int64_t)__builtin_amdgcn_readlane(upto, 63) * a.c.Hkv;
-            if (left >= sum) {
-                left -= sum;
-                continue;
-            }
-            const int who = __builtin_ctzll(__ballot((int64_t)upto * a.c.Hkv > left));
-            b = base + 64 * k + who;
-            sq.start = __builtin_amdgcn_readlane(q4[k].start, who);
-            sq.n = __builtin_amdgcn_readlane(q4[k].n, who);
-            sq.own = __builtin_amdgcn_readlane(q4[k].own, who);
-            per_head = __builtin_amdgcn_readlane(units, who);
-            left -= (int64_t)(__builtin_amdgcn_readlane(upto, who) - per_head) * a.c.Hkv;
-        }
-    }
-    if (b < 0) return;
-    const int h = (int)left / per_head;
-    int part = (int)left - h * per_head, tile = 0, parts;
-    OwnRange range;
-    for (;; ++tile) {
-        range = own_range<ROWS>(a, sq, tile);
-        parts = max((range.steps + len - 1) / len, 1);
-        if (part < parts) break;
-        part -= parts;
-    }
-    if (part == 0 && lane == 0) a.split[((int64_t)b * a.c.Hkv + h) * a.row_tiles + tile] = make_int2((int)unit64, parts);
-    const int begin = (int)((int64_t)range.steps * part / parts), end = (int)((int64_t)range.steps * (part + 1) / parts);
-    own_part<D, E5M2, MT, UNI>(x, sq, range, b, h, tile, begin, end, unit64, (v8bf*)buffer + wave * Q);
 }
 
 // Joins the pieces of the prefix and of a sequence's own: a workgroup per sequence, kv head and 4 of its rows; threads over channels (4 each),
@@ -629,8 +688,8 @@ cache_shared_join_kernel(SharedArgs x)
             y[u] = v4f{0.f, 0.f, 0.f, 0.f};
             if (i < n) {
                 const bool mine = i < own_n;
-                const float* p = mine ? a.pieces + (int64_t)(own_first + i) * (ROWS * (D + 2)) : x.pieces + (int64_t)(many_first + i - own_n) * (ROWS_MANY * (D + 2));
-                const int at = mine ? row % ROWS : many_row, all = mine ? ROWS : ROWS_MANY;
+                const float* p = mine ? a.pieces + (int64_t)(own_first + i) * x.piece_size : x.pieces + (int64_t)(many_first + i - own_n) * (ROWS_MANY * (D + 2));
+                const int at = mine ? row % ROWS : many_row, all = mine ? x.piece_rows : ROWS_MANY;
                 m2[u] = p[all * D + at];
                 l2[u] = p[all * D + all + at];
                 y[u] = *(const v4f*)(p + at * D + ch * 4);
@@ -671,7 +730,7 @@ cache_shared_join_kernel(SharedArgs x)
 // ---------------------------------------------------------------------------------------------------------------- host
 // Sizes of a call: row tiles of a sequence, items of both kinds and their pieces at most.
 struct SharedSizes {
-    int mt, more;
+    int mt, cus, more_own, piece_rows, piece_size;
     int64_t tiles, own_items, own_pieces, many_items, many_pieces, blocks;
     size_t bytes;
     bool fits;
@@ -681,25 +740,35 @@ static SharedSizes sizes_of(const CacheView& c, int B, int G, int N, int n_group
     SharedSizes z;
     const int64_t rows = (int64_t)N * G;
     z.mt = rows <= 16 ? 1 : 2;
+    z.piece_rows = (int)std::min<int64_t>(rows, 16 * z.mt);
+    z.piece_size = z.piece_rows * c.D + (2 * z.piece_rows + 3) / 4 * 4;
     z.tiles = (rows + 16 * z.mt - 1) / (16 * z.mt);
-    z.more = 2 * cache_cus();                     // as many as the chip holds
+    z.cus = cache_cus();
     z.own_items = (int64_t)B * c.Hkv * z.tiles;
-    z.own_pieces = z.more * WAVES + z.own_items;
+    z.more_own = (int)std::min<int64_t>(std::max<int64_t>(2 * z.own_items, 8 * z.cus), 16 * z.cus);
+    z.own_pieces = z.more_own + z.own_items + 16;
     z.many_items = ((int64_t)B * rows / ROWS_MANY + n_groups + 1) * c.Hkv;
-    z.many_pieces = z.more + (B * rows / ROWS_MANY + std::min(n_groups, B) + 1) * (int64_t)c.Hkv;
-    z.blocks = z.many_pieces + (z.own_items + WAVES - 1) / WAVES + 16;
-    z.bytes = (size_t)((z.own_pieces * 16 * z.mt + z.many_pieces * ROWS_MANY) * (c.D + 2) * 4 + (z.own_items + z.many_items) * 8);
+    z.many_pieces = 2 * (z.cus + (B * rows / ROWS_MANY + std::min(n_groups, B) + 1) * (int64_t)c.Hkv);
+    z.blocks = z.many_pieces + 32 + std::min<int64_t>((z.own_pieces + WAVES - 1) / WAVES, 2 * z.cus);
+    z.bytes = (size_t)((z.own_pieces * z.piece_size + z.many_pieces * ROWS_MANY * (c.D + 2)) * 4 + (z.own_items + z.many_items) * 8);
     z.fits = z.blocks * 256 <= 0xffffffffLL && (int64_t)B * c.Hkv * ((rows + 3) / 4) <= 0xffffffffLL / 512;
     return z;
 }
 
-// Whether sequences are taken together at all.
-static bool together(const SharedSizes& z, int G, int N, int n_groups) { return n_groups > 0 && (int64_t)N * G <= ROWS_MANY && z.fits; }
+// Whether sequences are taken together: where it saves reading this much once more, by the reach of the table (lengths are on the device), and
+// the rows of one sequence do not fill a tile anyway.
+constexpr int ROWS_TOGETHER = 64;
+constexpr double REPEATED = 1e8;
+static bool together(const SharedSizes& z, const CacheView& c, int B, int64_t rows, int n_groups, int window, int sinks)
+{
+    const int64_t capacity = (int64_t)c.max_pages << c.page_shift, reach = window ? std::min(capacity, (int64_t)window + sinks) : capacity;
+    return n_groups > 0 && rows <= ROWS_TOGETHER && (double)(B - n_groups) * reach * 2 * c.Hkv * c.D >= REPEATED && z.fits;
+}
 
 size_t cache_attn_shared_workspace(const CacheView& c, int B, int Hq, int N, int n_groups, int window, int sinks)
 {
     const SharedSizes z = sizes_of(c, B, Hq / c.Hkv, N, n_groups);
-    return together(z, Hq / c.Hkv, N, n_groups) ? z.bytes : cache_attn_workspace(c, B, Hq, N, window, sinks);
+    return together(z, c, B, (int64_t)N * (Hq / c.Hkv), n_groups, window, sinks) ? z.bytes : cache_attn_workspace(c, B, Hq, N, window, sinks);
 }
 
 template <int D, bool E5M2, int MT>
@@ -715,7 +784,7 @@ int launch_cache_attn_shared(const CacheView& c, const Rows& q, const Rows& out,
                              void* workspace, hipStream_t stream)
 {
     const SharedSizes z = sizes_of(c, s.B, Hq / c.Hkv, s.N, groups.n);
-    if (!together(z, Hq / c.Hkv, s.N, groups.n)) return launch_cache_attn(c, q, out, s, Hq, window, sinks, workspace, stream);
+    if (!together(z, c, s.B, (int64_t)s.N * (Hq / c.Hkv), groups.n, window, sinks)) return launch_cache_attn(c, q, out, s, Hq, window, sinks, workspace, stream);
     SharedArgs x = {};
     CacheAttnArgs& a = x.a;
     a.c = c;
@@ -730,11 +799,15 @@ int launch_cache_attn_shared(const CacheView& c, const Rows& q, const Rows& out,
     a.row_tiles = (int)z.tiles;
     x.g = groups;
     x.rows_per_seq = s.N * a.G;
-    x.more = z.more;
+    x.cus = z.cus;
+    x.more_own = z.more_own;
+    x.piece_rows = z.piece_rows;
+    x.piece_size = z.piece_size;
+    a.inv_g = (65536u + a.G - 1) / a.G;
     x.max_pieces = z.many_pieces;
     x.max_own = z.own_pieces;
     a.pieces = (float*)workspace;
-    x.pieces = a.pieces + z.own_pieces * 16 * z.mt * (c.D + 2);
+    x.pieces = a.pieces + z.own_pieces * z.piece_size;
     a.split = (int2*)(x.pieces + z.many_pieces * ROWS_MANY * (c.D + 2));
     x.split = a.split + z.own_items;
     auto pick = [&](auto D, auto F) { return z.mt == 1 ? launch_shared<D, F != 0, 1>(x, z, stream) : launch_shared<D, F != 0, 2>(x, z, stream); };

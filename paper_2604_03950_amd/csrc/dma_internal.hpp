@@ -89,7 +89,7 @@ int launch_cache_attn(const CacheView& c, const Rows& q, const Rows& out, const 
 size_t cache_attn_workspace(const CacheView& c, int B, int Hq, int N, int window, int sinks);
 
 // Pages that several sequences hold (dma_cache_pages.hip).  refs: table entries per page.
-constexpr int FORK_ROWS_MAX = 16384;
+constexpr int FORK_ROWS_MAX = 8192;
 int launch_kv_fork(const CacheView& c, int* refs, int B, const int* src, const int* length, hipStream_t stream);
 int launch_kv_reserve(const CacheView& c, int* refs, const Spans& s, int* missing, int* workspace, hipStream_t stream);
 int64_t reserve_pages(const CacheView& c, int N);          // that N tokens can touch

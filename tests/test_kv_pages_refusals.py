@@ -35,7 +35,7 @@ def test_caches(lib, fields, code):
 def test_other_arguments(lib):
     for kw in (dict(refs=None), dict(refs=FAKE + 2), dict(src=None), dict(src=FAKE + 1), dict(length=FAKE + 2), dict(B=-1)):
         assert fork(lib, **kw) == INVALID, kw
-    assert fork(lib, B=16385) == UNSUPPORTED
+    assert fork(lib, B=8193) == UNSUPPORTED
     for kw in (dict(refs=None), dict(refs=FAKE + 2), dict(start=None), dict(start=FAKE + 2), dict(n=FAKE + 1), dict(missing=None), dict(missing=FAKE + 2), dict(B=-1), dict(N=-1),
                dict(ws=None), dict(ws=FAKE + 2), dict(size=15)):
         assert reserve(lib, **kw) == INVALID, kw
