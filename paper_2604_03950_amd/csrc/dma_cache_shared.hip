@@ -437,8 +437,8 @@ DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& ran
 }
 
 constexpr int MIN_MANY = 2, MIN_OWN = 4;     // steps of a part at least
-// What the sequences' own parts take of a CU's time beside a prefix's part, in steps of that: to begin with, and per step.
-constexpr float OWN_FIRST = 4.5f, OWN_STEP = 0.9f;
+// What the sequences' own parts take of a CU's time beside a prefix's part, in steps of that: until a late part begins, and per step.
+constexpr float OWN_FIRST = 6.f, OWN_STEP[2] = {0.6f, 0.9f};      // tiles of 16 and of 32 rows
 // Of the steps that two parts of prefixes do side by side on a CU, those of the one that began later (the SIMDs prefer older waves).
 constexpr float LATE = 0.42f;
 constexpr float MIN_LATE = 3.f;              // steps of a late part at least
@@ -534,9 +534,9 @@ cache_shared_kernel(SharedArgs x)
         share = (int)((int64_t)share * all / x.cus) + 1;
         all = count();
     }
-    // A CU holds two workgroups.  A part of the prefixes for each goes first, and the sequences' own parts pass through the other place; behind them
-    // that place takes what is left of each part, so much that both end together.
-    const float each = many / (float)max(all, 1), own_time = OWN_FIRST + OWN_STEP * own_steps / (float)x.cus;
+    // A CU holds two workgroups.  One takes the early steps of a prefix's part; the other takes sequences' own parts and, behind them, the part's late
+    // steps, so many that both end together.
+    const float each = many / (float)max(all, 1), own_time = OWN_FIRST + OWN_STEP[MT - 1] * own_steps / (float)x.cus;
     float early = 1.f;
     if (LATE * (each - own_time) > MIN_LATE) early = 1.f - LATE * (1.f - own_time / each);
     const bool two = early < 1.f;
@@ -593,7 +593,7 @@ cache_shared_kernel(SharedArgs x)
                         left -= (__builtin_amdgcn_readlane(upto[k], who) - per_head) * a.c.Hkv;
                     }
                 }
-                if (b < 0) return;
+                if (b < 0) break;
                 const int h = left / per_head;
                 int part = left - h * per_head, tile = 0, parts;
                 OwnRange range;
@@ -607,10 +607,10 @@ cache_shared_kernel(SharedArgs x)
                 const int begin = (int)((int64_t)range.steps * part / parts), end = (int)((int64_t)range.steps * (part + 1) / parts);
                 own_part<D, E5M2, MT, UNI>(x, sq, range, b, h, tile, begin, end, unit, (v8bf*)buffer + wave * Q);
             }
-            return;
+            __syncthreads();                                      // (the queries of every wave have been read)
         }
+        // ... and behind them, or at once where there are none left, the late part of a prefix
         if (!two) return;
-        p -= own_blocks;
     }
     // a part of a prefix.  Workgroups next to each other in the list on the same XCD: they read the same keys
     const int at = p % 8 * per + p / 8;
