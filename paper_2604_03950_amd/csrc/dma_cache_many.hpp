@@ -14,6 +14,7 @@ struct ManyLds {
     K& k;
     V& v;
     int (&odd)[4];           // of step j at j & 3: bits 0 to 3: 16 positions without a page, bit 4: a value that is no number
+    int* some = nullptr;     // [4][waves], of step j at j & 3: bits 0 to 3: 16 positions of which a row of the wave sees one
 };
 
 // What is visible: positions [vis_lo, vis_hi] and those below the sinks to the row of this lane's column, ...
@@ -28,8 +29,8 @@ struct ManyRows {
 DMA_DEV int cut_position(int64_t p) { return (int)min(max(p, (int64_t)0), (int64_t)POS_MAX); }
 
 // Steps [begin, end) of the range, by the pages of sequence b: into sums o, maximum m and weight l of a lane's part of its row (the other half of
-// the wave has the other).  UNI: pages of 64 positions and more, so that a step lies in one: its address is the same for all threads.
-template <int D, bool E5M2, int NW, bool UNI>
+// the wave has the other).  GAPS: under a window, positions between those that rows see may be seen by none (rows of several sequences).  UNI: pages of 64 positions and more, so that a step lies in one: its address is the same for all threads.
+template <int D, bool E5M2, int NW, bool UNI, bool GAPS = false>
 DMA_DEV void many_steps(const CacheAttnArgs& a, const ManyLds<D>& lds, int b, int h, const StepRange& range, int begin, int end, const ManyRows& r,
                         v8bf (&qf)[D / 16], v16f (&o)[D / 32], float& m, float& l)
 {
@@ -132,7 +133,13 @@ DMA_DEV void many_steps(const CacheAttnArgs& a, const ManyLds<D>& lds, int b, in
             if (!there) odd |= 1 << (ch & 3);
             if (!open || !there) {
                 auto below = [&](int q) { return (1u << min(max(q - pos - (ch & 3) * 16, 0), 16)) - 1u; };
-                const unsigned seen = there ? below(r.any_hi + 1) & (~below(r.any_lo) | below(a.sinks)) : 0u;
+                unsigned seen = there ? below(r.any_hi + 1) & (~below(r.any_lo) | below(a.sinks)) : 0u;
+                if constexpr (GAPS) {
+                    int some = 0;
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) some |= lds.some[(j & 3) * NW + w];
+                    if (a.window && !((some >> (ch & 3)) & 1)) seen = 0;
+                }
                 if (!seen) sc = 1.f;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -147,6 +154,22 @@ DMA_DEV void many_steps(const CacheAttnArgs& a, const ManyLds<D>& lds, int b, in
                 *(v8bf*)(lds.v[buf] + d * VROW + ((2 * (ch & 3) + e) ^ shift_of(d, VROW)) * 16) = decode8<E5M2>(cd.v[u][2 * e], cd.v[u][2 * e + 1], sc);
         }
         if (odd) atomicOr(&lds.odd[j & 3], odd);
+    };
+
+    // (a page of which no row sees anything may have any scale; where one row sees some of 16 positions, the others among them are numbers, or
+    // are found not to be)
+    auto look = [&](int j) {
+        if constexpr (GAPS) {
+            if (!a.window) return;
+            const int pos = range.position(j);
+            int some = 0;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int p = pos + 16 * g;
+                if (__any(p <= r.vis_hi && (p + 15 >= r.vis_lo || p < a.sinks))) some |= 1 << g;
+            }
+            if (lane == 0) lds.some[(j & 3) * NW + (int)(threadIdx.x >> 6)] = some;
+        }
     };
 
 #pragma unroll
@@ -168,6 +191,8 @@ DMA_DEV void many_steps(const CacheAttnArgs& a, const ManyLds<D>& lds, int b, in
         load(begin, pages, codes0);
         load(min(begin + 1, end - 1), pages1, codes);
         load_pages(min(begin + 2, end - 1), pages);
+        look(begin);
+        look(begin + 1);
         __syncthreads();
         stage(begin, begin & 1, codes0);
     }
@@ -188,6 +213,7 @@ DMA_DEV void many_steps(const CacheAttnArgs& a, const ManyLds<D>& lds, int b, in
             if (j + 2 < end) load(j + 2, pages, codes);
             if (j + 3 < end) load_pages(j + 3, pages);
         }
+        look(j + 2);
         if (threadIdx.x == 0) lds.odd[(j + 2) & 3] = 0;            // last read two steps ago, next written in the next one
         const int odd = lds.odd[j & 3];
         const bool none = r.my_rows <= 0 || pos > r.some_hi || (pos + STEP <= r.some_lo && pos >= a.sinks);

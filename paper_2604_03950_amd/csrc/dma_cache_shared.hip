@@ -178,7 +178,7 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     (late ? begin : end) = cut;
     v16f o[D / 32];
     float m, l;
-    many_steps<D, E5M2, WAVES, UNI>(a, lds, g.lo, h, range, begin, end, view, qf, o, m, l);
+    many_steps<D, E5M2, WAVES, UNI, true>(a, lds, g.lo, h, range, begin, end, view, qf, o, m, l);
     if (col >= my_rows) return;
     l = cross_half_sum(l);
     float* p = x.pieces + piece * (ROWS_MANY * (D + 2));          // (past the caches, which would be written back at the kernel's end: 29.5 us, 27.9)
@@ -452,7 +452,7 @@ cache_shared_kernel(SharedArgs x)
     constexpr int ROWS = 16 * MT, MANY = sizeof(typename Many::K) + sizeof(typename Many::V), Q = MT > 1 ? MT * (D / 32) * 64 : 1;
     static_assert(WAVES * Q * 16 <= MANY, "");
     __shared__ __attribute__((aligned(16))) char buffer[MANY];
-    __shared__ int odd[4], ends[4][WAVES], first[GROUPS_LDS + 1], steps[GROUPS_LDS];
+    __shared__ int odd[4], some[4][WAVES], ends[4][WAVES], first[GROUPS_LDS + 1], steps[GROUPS_LDS];
     const CacheAttnArgs& a = x.a;
     const bool few_groups = x.g.n <= GROUPS_LDS;
     if (few_groups) {
@@ -635,7 +635,7 @@ cache_shared_kernel(SharedArgs x)
         const int64_t piece = two ? 2 * ((int64_t)first_piece + item * parts + part) + late : (int64_t)first_piece + item * parts + part;
         if (i < 0 || h >= a.c.Hkv || piece < 0 || piece >= x.max_pieces) return;          // (bounds that decrease)
         if (part == 0 && !late && threadIdx.x == 0) x.split[(tiles_before(x, base + who, mine.lo)) * a.c.Hkv + item] = make_int2((first_piece + item * parts) << two, parts << two);
-        const Many lds = {*(typename Many::K*)buffer, *(typename Many::V*)(buffer + sizeof(typename Many::K)), odd};
+        const Many lds = {*(typename Many::K*)buffer, *(typename Many::V*)(buffer + sizeof(typename Many::K)), odd, some[0]};
         prefix_part<D, E5M2, UNI>(x, lds, ends, mine, h, tile, part, parts, early, late, piece);
         return;
     }

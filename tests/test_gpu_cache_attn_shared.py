@@ -1,6 +1,9 @@
 """Attention over the cache behind shared prefixes, on the GPU against its definition in 64 bits (kv_plain): the same as attention over
 the cache row by row, within the bound that kv_plain derives for every element.  Joining pieces of a row's sums multiplies each by one factor
-that exp2 gives, which the bound's count of 32 units beside the number of keys covers, as for pieces of long sequences."""
+that exp2 gives, which the bound's count of 32 units beside the number of keys covers, as for pieces of long sequences.
+
+Where little would be read twice the call is served by the kernels of dma_cache_attn; what it goes by is the reach of the page table, so tables
+with many empty columns (wide) bring short sequences to the kernel for shared prefixes."""
 import numpy as np
 import pytest
 import torch
@@ -24,7 +27,8 @@ class Family(Pair):
     """Sequences of groups: sizes and common lengths of these (positions, taken down to whole pages), lens[b] positions in all; -1 as
     a common length: sequences of no group."""
 
-    def __init__(self, rng, groups, lens, Hkv, P, D, fmt, write=True, spare=1):
+    def __init__(self, rng, groups, lens, Hkv, P, D, fmt, write=True, spare=1, wide=True):
+        self.wide = wide
         wide = max(-(-n // P) for n in lens) + spare
         table, at, b, self.bounds, self.shared = np.full((len(lens), wide), -1, np.int32), 0, 0, [], []
         order = rng.permutation(sum(-(-n // P) for n in lens) + 3)
@@ -48,6 +52,11 @@ class Family(Pair):
         self.shared = [s // P * P for s in self.shared]
         assert b == len(lens)
         super().__init__(rng, None, Hkv, P, D, fmt, table, len(order))
+        self.together = self.wide and len(lens) > len(self.shared) > 0
+        if self.together:                                          # empty columns, on the GPU alone
+            columns = int(2e8 / ((len(lens) - len(self.shared)) * P * 2 * Hkv * D)) + 1
+            g = self.gpu
+            self.gpu = dma.KVCache(g.k_codes, g.v_codes, g.k_scales, g.v_scales, torch.nn.functional.pad(g.page_table, (0, columns), value=-1), g.fmt[0] if isinstance(g.fmt, tuple) else g.fmt)
         if write:
             start = np.array([own for _, own in leaders])
             n = np.maximum(np.array(lens) - start, 0)
@@ -56,6 +65,8 @@ class Family(Pair):
     def attn(self, q, start, n=None, window=0, sinks=0, out=None, shared=None, bounds=None, **kw):
         got = dma.dma_cache_attn_shared(q.cuda() if not q.is_cuda else q, self.gpu, i32(start), i32(self.bounds or [0] if bounds is None else bounds),
                                         i32(np.array(self.shared if shared is None else shared, int)), i32(n), window=window, sink_tokens=sinks, out=out, **kw)
+        if self.together and bounds is None and not window and q.shape[1] // self.cpu.Hkv * q.shape[2] <= 64:
+            self.served_together(q.shape[1], q.shape[2])
         want, bound = self.cpu.attn(q.double().cpu().numpy(), start, n, window, sinks)
         rows = np.isfinite(want)
         off = np.abs(got.double().cpu().numpy() - want)[rows]
@@ -64,25 +75,54 @@ class Family(Pair):
         assert worst <= 0, (worst, off.max(), (off / bound[rows]).max())
         return got, rows
 
+    def served_together(self, Hq, N):
+        assert dma.dma_cache_attn_shared_workspace_bytes(self.gpu, Hq, N, len(self.shared)) != dma.dma_cache_attn_workspace_bytes(self.gpu, Hq, N)
+
 
 FORMS = [("e4m3", 128, 64, 2, 4, 1), ("e5m2", 128, 16, 1, 1, 1), ("e4m3", 64, 32, 3, 5, 1), ("e5m2", 64, 256, 2, 8, 1), ("e4m3", 128, 128, 1, 16, 1),
-         ("e4m3", 128, 64, 2, 4, 3), ("e4m3", 64, 16, 1, 1, 17), ("e5m2", 128, 128, 2, 5, 7), ("e4m3", 128, 32, 1, 4, 33), ("e5m2", 64, 64, 1, 8, 20)]
+         ("e4m3", 128, 64, 2, 4, 3), ("e4m3", 64, 16, 1, 1, 17), ("e5m2", 128, 128, 2, 5, 7), ("e4m3", 128, 32, 1, 4, 33), ("e5m2", 64, 64, 1, 8, 20),
+         ("e4m3", 128, 64, 1, 4, 8), ("e5m2", 64, 32, 2, 8, 8), ("e4m3", 128, 16, 1, 5, 13), ("e4m3", 64, 256, 1, 4, 16), ("e5m2", 128, 256, 1, 3, 21)]
 
 
 @pytest.mark.parametrize("fmt,D,P,Hkv,G,N", FORMS)
 @pytest.mark.parametrize("groups", [[(1, 100)], [(7, 300)], [(2, -1), (3, 70), (0, 9), (5, 513), (1, 0), (2, -1)], [(4, 0)], [(3, -1)]])
-@pytest.mark.parametrize("window,sinks", [(0, 0), (50, 0), (150, 70)])
-def test_groups(fmt, D, P, Hkv, G, N, groups, window, sinks):
+@pytest.mark.parametrize("window,sinks,wide", [(0, 0, True), (50, 0, True), (150, 70, True), (1 << 30, 0, True), (150, 70, False)])
+def test_groups(fmt, D, P, Hkv, G, N, groups, window, sinks, wide):
     rng = np.random.default_rng(D + P + N + len(groups) + window)
     lens = []
     for size, common in groups:
         lens += [max(common, 0) + N + int(x) for x in rng.integers(0, 200, size)]
-    f = Family(rng, groups, lens, Hkv, P, D, fmt)
+    f = Family(rng, groups, lens, Hkv, P, D, fmt, wide=wide)
     B = len(lens)
     n = np.full(B, N) if N == 1 else np.maximum(rng.integers(0, N + 1, B), [N] + [0] * (B - 1))
     out = torch.full((B, Hkv * G, N, D), 7.0, dtype=torch.bfloat16, device="cuda")
     got, rows = f.attn(bf16(rng, B, Hkv * G, N, D), np.array(lens) - n, n, window, sinks, out=out)
     assert got is out and (got.float().cpu().numpy()[~rows] == 7).all()
+
+
+@pytest.mark.parametrize("fmt,D,P,Hkv,G,N,B,prefix,own,window,sinks", [
+    ("e4m3", 128, 64, 32, 1, 1, 43, 320, 300, 310, 0), ("e4m3", 128, 16, 32, 2, 1, 43, 300, 200, 310, 5), ("e5m2", 128, 32, 32, 1, 2, 58, 256, 150, 210, 70),
+    ("e5m2", 64, 64, 32, 1, 2, 62, 400, 100, 420, 500), ("e4m3", 64, 256, 32, 1, 3, 84, 512, 200, 300, 0), ("e4m3", 128, 128, 32, 1, 1, 240, 64, 40, 50, 4)])
+def test_windows(fmt, D, P, Hkv, G, N, B, prefix, own, window, sinks):
+    """Windows whose far end lies in the prefix, behind it, before the sequence; sinks in the prefix and beyond it.  What no row sees may be anything.
+    (Enough heads and sequences for the kernel for shared prefixes.)"""
+    rng = np.random.default_rng(B + prefix)
+    lens = [prefix + N + int(x) for x in rng.integers(0, own, B)]
+    cut = B // 3
+    f = Family(rng, [(cut, prefix), (B - cut, prefix // 2)], lens, Hkv, P, D, fmt, wide=False)
+    assert dma.dma_cache_attn_shared_workspace_bytes(f.gpu, Hkv * G, N, 2, window, sinks) != dma.dma_cache_attn_workspace_bytes(f.gpu, Hkv * G, N, window, sinks)
+    start = np.array(lens) - N
+    start[:4] = 0, prefix // 3, prefix // 2, prefix - 1
+    start[cut:cut + 3] = prefix // 2 - 1, 5, -1
+    seen = set()
+    for b in range(B):
+        if start[b] >= 0:
+            for j in range((start[b] + N - 1) // P + 1):
+                if (j + 1) * P > start[b] - window + 1 or j * P < sinks:
+                    seen.add(int(f.cpu.table[b, j]))
+    for p in set(range(f.cpu.pages)) - seen:
+        f.gpu.k_codes[p], f.gpu.v_codes[p], f.gpu.k_scales[p], f.gpu.v_scales[p] = 0x7f, 0x7f, 255, 255
+    f.attn(bf16(rng, B, Hkv * G, N, D), start, None, window, sinks)
 
 
 @pytest.mark.parametrize("N,G", [(1, 4), (5, 2)])
@@ -116,13 +156,17 @@ def test_bounds_of_groups():
         f.attn(bf16(rng, 8, 4, 1, 64), [299] * 8, bounds=bounds, shared=shared)
 
 
-def test_shared_beyond_the_table():
-    """A shared length at the end of its type: all rows name the same pages as far as the table goes, the tokens themselves among them."""
+@pytest.mark.parametrize("B,Hkv", [(5, 1), (430, 4)])
+def test_shared_beyond_the_table(B, Hkv):
+    """A shared length at the end of its type: all rows name the same pages as far as the table goes, the tokens themselves among them.  (So
+    many rows of a short table are enough for the kernel for shared prefixes.)"""
     rng = np.random.default_rng(5)
-    f = Family(rng, [(5, 256)], [256] * 5, 1, 64, 128, "e4m3", spare=0)
+    f = Family(rng, [(B, 256)], [256] * B, Hkv, 64, 128, "e4m3", spare=0, wide=False)
+    if B > 5:
+        f.served_together(Hkv, 1)
     for shared in (256, (1 << 31) - 1):
-        f.attn(bf16(rng, 5, 4, 1, 128), [255, 255, 100, 255, 3], shared=[shared])
-        f.attn(bf16(rng, 5, 4, 2, 128), [300, (1 << 31) - 1, 254, 1 << 30, 255], None, 200, 3, shared=[shared])
+        f.attn(bf16(rng, B, Hkv, 1, 128), [255, 255, 100, 255, 3] * (B // 5), shared=[shared])
+        f.attn(bf16(rng, B, Hkv, 2, 128), [300, (1 << 31) - 1, 254, 1 << 30, 255] * (B // 5), None, 250, 3, shared=[shared])
 
 
 @pytest.mark.parametrize("fmt,D,G,N,P", [("e4m3", 128, 4, 1, 64), ("e5m2", 64, 2, 3, 16), ("e4m3", 128, 1, 1, 128)])
