@@ -321,6 +321,7 @@ size_t dma_kv_reserve_workspace_bytes(const dma_kv_cache* cache, int B, int N);
  *   moved_i32  [num_pages] int32, device, 4-byte aligned, out: where the page lies now, -1 for free ones (what a caller needs for other
  *              tables of page numbers).
  *   workspace  device, 8-byte aligned, at least dma_kv_compact_workspace_bytes(...) bytes; as for dma_cache_attn.
+ *   B = 0 is a no-op: nothing is written, used and moved neither.
  */
 int dma_kv_compact(const dma_kv_cache* cache, void* refs_i32, int B, void* used_i32, void* moved_i32, void* workspace, size_t workspace_bytes,
                    void* stream);
@@ -330,10 +331,11 @@ size_t dma_kv_compact_workspace_bytes(const dma_kv_cache* cache);
  * dma_cache_attn for sequences that share a long prefix, whose keys and values are read once for all of them.
  *   n_groups >= 0; group_start [n_groups + 1] int32, device, 4-byte aligned, not decreasing: group g holds the sequences group_start[g] up to
  *   group_start[g + 1] (not included), of the B.  A sequence may be in no group.
- *   shared [n_groups] int32, device, 4-byte aligned: the positions [0, shared[g]) of all sequences of group g are the same: their rows of the table
- *   name the same pages there (or pages that hold the same).  What is read for all is read by the first row of the group.
+ *   shared [n_groups] int32, device, 4-byte aligned: the positions [0, shared[g]) of all sequences of group g that have tokens are the same: their rows
+ *   of the table name the same pages there (or pages that hold the same).  Below 1: none.
  *   Everything else is as for dma_cache_attn, and so is what the call computes; the order of its sums differs, and so may the last bits.
  * A group_start that decreases gives unspecified results, never a fault.  With n_groups = 0 the two arrays are not looked at (may be NULL).
+ * n_groups > 2^24: DMA_ERR_UNSUPPORTED.
  */
 int dma_cache_attn_shared(const dma_kv_cache* cache, const dma_rows* q, const dma_rows* out, int B, int Hq, int N, const void* start_i32,
                           const void* n_tokens_i32, int n_groups, const void* group_start_i32, const void* shared_i32, int window, int sink_tokens,

@@ -472,6 +472,8 @@ def dma_kv_compact(cache: KVCache, refs: torch.Tensor, *, used: torch.Tensor | N
     and int32 [pages], where each page lies now (-1: free).  workspace: contiguous uint8 of at least
     dma_kv_compact_workspace_bytes(cache) bytes, 8-byte aligned, for one call at a time; by default one is allocated."""
     stream = _cache_stream(cache)
+    if cache.B == 0:
+        raise ValueError("a cache without sequences has nothing that says what its pages hold")
     pages = cache._c.num_pages
     pr = _ints(cache, refs, pages, "refs")
     if used is None:
@@ -495,8 +497,9 @@ def dma_kv_compact_workspace_bytes(cache: KVCache) -> int:
 def dma_cache_attn_shared(q: torch.Tensor, cache: KVCache, start: torch.Tensor, groups: torch.Tensor, shared: torch.Tensor,
                           n_tokens: torch.Tensor | None = None, *, window: int = 0, sink_tokens: int = 0, out: torch.Tensor | None = None,
                           workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """dma_cache_attn for sequences with common prefixes, each of which is read once: the sequences groups[g] .. groups[g + 1] - 1 have the
-    same pages for their first shared[g] positions (int32 [n + 1], not decreasing, and int32 [n], on the GPU).  Everything else as there."""
+    """dma_cache_attn for sequences with common prefixes, each of which is read once: those of the sequences groups[g] .. groups[g + 1] - 1
+    that have tokens have the same pages for their first shared[g] positions (int32 [n + 1], not decreasing, and int32 [n], on the GPU).
+    Everything else as there."""
     stream = _cache_stream(cache)
     ps = _counts(cache, start, "start")
     pn = None if n_tokens is None else _counts(cache, n_tokens, "n_tokens")

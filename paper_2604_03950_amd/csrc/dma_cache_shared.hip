@@ -123,7 +123,7 @@ DMA_DEV float wave_sum(float v)
 
 // One workgroup's part of the prefixes: 128 rows of a group, some of their steps, into piece `piece`.
 template <int D, bool E5M2, bool UNI>
-DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)[4][WAVES], const Bounds& g, int h, int tile, int part, int parts, float early, bool late, int64_t piece)
+DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)[5][WAVES], const Bounds& g, int h, int tile, int part, int parts, float early, bool late, int64_t piece)
 {
     const CacheAttnArgs& a = x.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
@@ -141,6 +141,9 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     }
     const SeqInfo sq = seq_of(a, b);
     const bool exists = tok < sq.n && col < my_rows;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)                           // (rows that do not exist may hold anything, and share the wave's maxima)
+        qf[ks] = exists ? qf[ks] : __builtin_bit_cast(v8bf, v4i{0, 0, 0, 0});
     // ---- what is visible.  Rows that do not exist have no say in it
     const int64_t at = (int64_t)sq.start + tok;
     ManyRows view;
@@ -151,7 +154,10 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     view.some_hi = wave_max(view.vis_hi);
     view.all_lo = wave_max(view.vis_lo);
     view.some_lo = -wave_max(exists ? -view.vis_lo : -POS_MAX);
+    // the table of the first sequence that has tokens: one that ended may have none of the pages any more
+    const int first_b = wave_max(exists ? -b : -0x7fffffff);
     if (lane == 0) {
+        ends[4][wave] = first_b;
         ends[0][wave] = view.all_hi;
         ends[1][wave] = view.some_hi;
         ends[2][wave] = view.all_lo;
@@ -166,6 +172,7 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     view.any_hi = __builtin_amdgcn_readfirstlane(view.any_hi);
     view.wg_lo = __builtin_amdgcn_readfirstlane(view.wg_lo);
     view.any_lo = __builtin_amdgcn_readfirstlane(view.any_lo);
+    const int by = min(-__builtin_amdgcn_readfirstlane(max(max(ends[4][0], ends[4][1]), max(ends[4][2], ends[4][3]))), a.s.B - 1);
     // ---- the steps: of the shared ones, those that a row sees
     const int hi = min(view.any_hi + 1, g.steps * STEP), lo = min(view.any_lo, hi);
     StepRange range;
@@ -178,7 +185,7 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     (late ? begin : end) = cut;
     v16f o[D / 32];
     float m, l;
-    many_steps<D, E5M2, WAVES, UNI, true>(a, lds, g.lo, h, range, begin, end, view, qf, o, m, l);
+    many_steps<D, E5M2, WAVES, UNI, true>(a, lds, by, h, range, begin, end, view, qf, o, m, l);
     if (col >= my_rows) return;
     l = cross_half_sum(l);
     float* p = x.pieces + piece * (ROWS_MANY * (D + 2));          // (past the caches, which would be written back at the kernel's end: 29.5 us, 27.9)
@@ -452,7 +459,7 @@ cache_shared_kernel(SharedArgs x)
     constexpr int ROWS = 16 * MT, MANY = sizeof(typename Many::K) + sizeof(typename Many::V), Q = MT > 1 ? MT * (D / 32) * 64 : 1;
     static_assert(WAVES * Q * 16 <= MANY, "");
     __shared__ __attribute__((aligned(16))) char buffer[MANY];
-    __shared__ int odd[4], some[4][WAVES], ends[4][WAVES], first[GROUPS_LDS + 1], steps[GROUPS_LDS];
+    __shared__ int odd[4], some[4][WAVES], ends[5][WAVES], first[GROUPS_LDS + 1], steps[GROUPS_LDS];
     const CacheAttnArgs& a = x.a;
     const bool few_groups = x.g.n <= GROUPS_LDS;
     if (few_groups) {

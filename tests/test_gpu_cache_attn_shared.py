@@ -265,6 +265,24 @@ def test_unseen_places_may_hold_anything(N, fill):
     f.attn(bf16(rng, B, 4, N, D), start, None, 150)
 
 
+def test_sequences_that_ended():
+    """Sequences without tokens have no say: the first of a group has lost its pages, queries of rows that do not exist are NaN and infinite."""
+    rng = np.random.default_rng(48)
+    f = Family(rng, [(3, 320), (60, 512)], [400] * 3 + [600 + i for i in range(60)], 1, 32, 128, "e4m3")
+    gone = [0, 3, 4, 5, 60, 62]
+    f.cpu.table[gone] = -1
+    f.gpu.page_table[gone] = -1
+    start, n = np.array([399, 398, 397] + [598 + i for i in range(60)]), np.full(63, 2)
+    start[gone[:3]] = -1
+    n[gone[3:]] = 0
+    n[30:50] = 1
+    q = bf16(rng, 63, 4, 2, 128)
+    clean, _ = f.attn(q, start, n)
+    q[gone], q[30:40, :, 1], q[40:50, :, 1] = float("nan"), float("inf"), float("nan")
+    got = dma.dma_cache_attn_shared(q.cuda(), f.gpu, i32(start), i32(f.bounds), i32(f.shared), i32(n))
+    assert torch.equal(got, clean)
+
+
 def test_strides_and_streams():
     """Queries and results as views of larger tensors, on a stream of their own."""
     rng = np.random.default_rng(43)

@@ -105,6 +105,9 @@ def test_binding_checks_shapes(handle, monkeypatch):  # noqa: F811
     for bad in (on_gpu(3, 8, 64), on_gpu(3, 8, 4, 128), on_gpu(2, 8, 4, 64), torch.zeros((3, 8, 4, 64), dtype=torch.bfloat16)):
         with pytest.raises(ValueError):
             dma.dma_cache_attn_shared(bad, handle, three, i32(2), i32(1), out=q)
+    empty = dma.KVCache(handle.k_codes, handle.v_codes, handle.k_scales, handle.v_scales, i32(0, 5))
+    with pytest.raises(ValueError):
+        dma.dma_kv_compact(empty, refs, used=i32(1), moved=i32(4))
     monkeypatch.setattr(dma, "_current_device", lambda: 1)     # another device is the current one
     for call in (lambda: dma.dma_kv_fork(handle, refs, three), lambda: dma.dma_kv_reserve(handle, refs, three, 1), lambda: dma.dma_kv_compact(handle, refs),
                  lambda: dma.dma_cache_attn_shared(q, handle, three, i32(2), i32(1))):
