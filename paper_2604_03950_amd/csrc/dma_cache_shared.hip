@@ -23,7 +23,8 @@ struct SharedArgs {
     int piece_rows;          // of a sequence's own piece: at most 16 * MT
     int piece_size;          // in floats: sums, then maxima and weights, up to a multiple of 4
     float* pieces;           // of the prefixes: per workgroup [128][D] sums, [128] maxima, [128] weights
-    int2* split;             // per kv head and row tile: the first piece and how many
+    int4* where;             // per sequence and kv head, for the tile that holds its first rows and the next one: first piece, how many (0: it
+                             // shares nothing), place of the sequence's first row in the tile
     int64_t max_pieces, max_own;
     int cus;
     int more_own;            // waves beyond one for each row tile of the sequences: tiles in several parts
@@ -34,16 +35,6 @@ struct Bounds {
     int steps;               // that they share
 };
 DMA_DEV int shared_steps(const SharedArgs& x, int shared) { return max(min(shared, x.a.capacity), 0) / STEP; }
-DMA_DEV Bounds bounds_of(const SharedArgs& x, int g)
-{
-    Bounds r;
-    r.lo = min(max(x.g.first[g], 0), x.a.s.B);
-    r.hi = min(max(x.g.first[g + 1], r.lo), x.a.s.B);
-    r.steps = shared_steps(x, x.g.shared[g]);
-    return r;
-}
-// Items of the groups lie in order; this many at most before those of group g, whose first sequence is lo.
-DMA_DEV int64_t tiles_before(const SharedArgs& x, int g, int lo) { return (int64_t)lo * x.rows_per_seq / ROWS_MANY + g; }
 
 // The group of sequence b: the last one that does not begin behind it.  first(g): where group g begins.
 template <typename F>
@@ -123,7 +114,7 @@ DMA_DEV float wave_sum(float v)
 
 // One workgroup's part of the prefixes: 128 rows of a group, some of their steps, into piece `piece`.
 template <int D, bool E5M2, bool UNI>
-DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)[5][WAVES], const Bounds& g, int h, int tile, int part, int parts, float early, bool late, int64_t piece)
+DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)[5][WAVES], const Bounds& g, int h, int tile, int part, int parts, float early, bool late, int64_t piece, int2 pieces)
 {
     const CacheAttnArgs& a = x.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
@@ -132,7 +123,9 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
     // ---- this lane's row: sequence, token and head
     const int64_t r = min((int64_t)tile * ROWS_MANY + wave * 32 + col, all_rows - 1);
     const int b = g.lo + (int)((unsigned)r / (unsigned)x.rows_per_seq), in_seq = (int)((unsigned)r % (unsigned)x.rows_per_seq);
-    const int tok = token_of<true>(a, in_seq);
+    const int tok = token_of<true>(a, in_seq), place = wave * 32 + col;
+    if (part == 0 && !late && half == 0 && col < my_rows && (in_seq == 0 || place == 0))
+        x.where[((int64_t)b * a.c.Hkv + h) * 2 + (in_seq != 0)] = make_int4(pieces.x, pieces.y, place - in_seq, 0);
     v8bf qf[D / 16];
     {
         const char* qp = a.q.data + b * a.q.stride_batch + (h * a.G + in_seq - tok * a.G) * a.q.stride_head + tok * a.q.stride_token;
@@ -610,7 +603,11 @@ cache_shared_kernel(SharedArgs x)
                     if (ONE || part < parts) break;
                     part -= parts;
                 }
-                if (part == 0 && lane == 0) a.split[((int64_t)b * a.c.Hkv + h) * a.row_tiles + tile] = make_int2(unit, parts);
+                if (part == 0 && lane == 0) {
+                    const int64_t pair = (int64_t)b * a.c.Hkv + h;
+                    a.split[pair * a.row_tiles + tile] = make_int2(unit, parts);
+                    if (sq.own == 0) x.where[2 * pair] = make_int4(0, 0, 0, 0);
+                }
                 const int begin = (int)((int64_t)range.steps * part / parts), end = (int)((int64_t)range.steps * (part + 1) / parts);
                 own_part<D, E5M2, MT, UNI>(x, sq, range, b, h, tile, begin, end, unit, (v8bf*)buffer + wave * Q);
             }
@@ -641,9 +638,8 @@ cache_shared_kernel(SharedArgs x)
         const int item = h * n_tiles + tile;
         const int64_t piece = two ? 2 * ((int64_t)first_piece + item * parts + part) + late : (int64_t)first_piece + item * parts + part;
         if (i < 0 || h >= a.c.Hkv || piece < 0 || piece >= x.max_pieces) return;          // (bounds that decrease)
-        if (part == 0 && !late && threadIdx.x == 0) x.split[(tiles_before(x, base + who, mine.lo)) * a.c.Hkv + item] = make_int2((first_piece + item * parts) << two, parts << two);
         const Many lds = {*(typename Many::K*)buffer, *(typename Many::V*)(buffer + sizeof(typename Many::K)), odd, some[0]};
-        prefix_part<D, E5M2, UNI>(x, lds, ends, mine, h, tile, part, parts, early, late, piece);
+        prefix_part<D, E5M2, UNI>(x, lds, ends, mine, h, tile, part, parts, early, late, piece, make_int2((first_piece + item * parts) << two, parts << two));
         return;
     }
 }
@@ -657,30 +653,19 @@ cache_shared_join_kernel(SharedArgs x)
     constexpr int CH = D / 4, PG = T / (4 * CH), U = 8;
     const CacheAttnArgs& a = x.a;
     const int h = blockIdx.x % (unsigned)a.c.Hkv, b = blockIdx.x / (unsigned)a.c.Hkv;
+    const int r0 = blockIdx.y * 4, rr = threadIdx.x / CH % 4, ch = threadIdx.x % CH, pg = threadIdx.x / (4 * CH);
+    // ---- where the pieces are (within the workspace whatever the bounds of the groups say)
+    const int64_t pair = (int64_t)b * a.c.Hkv + h;
     const SeqInfo sq = seq_of(a, b);
-    const int rows = sq.n * a.G, r0 = blockIdx.y * 4, rr = threadIdx.x / CH % 4, ch = threadIdx.x % CH, pg = threadIdx.x / (4 * CH);
+    const int4 in0 = x.where[2 * pair], in1 = x.where[2 * pair + 1];
+    const int2 sp = a.split[pair * a.row_tiles + min(r0 + rr, x.rows_per_seq - 1) / ROWS];
+    const int rows = sq.n * a.G;
     if (r0 >= rows) return;
     const int row = min(r0 + rr, rows - 1);
-    // ---- where the pieces are
-    const int g = group_of([&](int i) { return x.g.first[i]; }, x.g.n, b);
-    int own_first, own_n, many_first = 0, many_n = 0, many_row = 0;
-    {
-        const int2 sp = a.split[((int64_t)b * a.c.Hkv + h) * a.row_tiles + row / ROWS];
-        // (within the workspace whatever the bounds of the groups say, here and below)
-        own_first = max(sp.x, 0);
-        own_n = (int)min((int64_t)max(sp.y, 0), max(x.max_own - own_first, (int64_t)0));
-    }
-    if (g >= 0) {
-        const Bounds r = bounds_of(x, g);
-        if (r.steps > 0) {
-            const int64_t in_group = (int64_t)(b - r.lo) * x.rows_per_seq + row;
-            const int n_tiles = (int)(((int64_t)(r.hi - r.lo) * x.rows_per_seq + ROWS_MANY - 1) / ROWS_MANY);
-            const int2 sp = x.split[tiles_before(x, g, r.lo) * a.c.Hkv + h * n_tiles + in_group / ROWS_MANY];
-            many_first = max(sp.x, 0);
-            many_n = (int)min((int64_t)max(sp.y, 0), max(x.max_pieces - many_first, (int64_t)0));
-            many_row = (int)(in_group % ROWS_MANY);
-        }
-    }
+    const int4 in = row + in0.z < ROWS_MANY ? in0 : in1;
+    const int own_first = max(sp.x, 0), own_n = (int)min((int64_t)max(sp.y, 0), max(x.max_own - own_first, (int64_t)0));
+    const int many_first = max(in.x, 0), many_row = (row + in.z) & (ROWS_MANY - 1);
+    const int many_n = in0.y == 0 ? 0 : (int)min((int64_t)max(in.y, 0), max(x.max_pieces - many_first, (int64_t)0));
     v4f o = {0.f, 0.f, 0.f, 0.f};
     float m = M_NONE, l = 0.f;
     const int n = own_n + many_n;
@@ -738,7 +723,7 @@ cache_shared_join_kernel(SharedArgs x)
 // Sizes of a call: row tiles of a sequence, items of both kinds and their pieces at most.
 struct SharedSizes {
     int mt, cus, more_own, piece_rows, piece_size;
-    int64_t tiles, own_items, own_pieces, many_items, many_pieces, blocks;
+    int64_t tiles, own_items, own_pieces, many_pieces, blocks;
     size_t bytes;
     bool fits;
 };
@@ -754,10 +739,9 @@ static SharedSizes sizes_of(const CacheView& c, int B, int G, int N, int n_group
     z.own_items = (int64_t)B * c.Hkv * z.tiles;
     z.more_own = (int)std::min<int64_t>(std::max<int64_t>(2 * z.own_items, 8 * z.cus), 16 * z.cus);
     z.own_pieces = z.more_own + z.own_items + 16;
-    z.many_items = ((int64_t)B * rows / ROWS_MANY + n_groups + 1) * c.Hkv;
     z.many_pieces = 2 * (z.cus + (B * rows / ROWS_MANY + std::min(n_groups, B) + 1) * (int64_t)c.Hkv);
     z.blocks = z.many_pieces + 32 + std::min<int64_t>((z.own_pieces + WAVES - 1) / WAVES, 2 * z.cus);
-    z.bytes = (size_t)((z.own_pieces * z.piece_size + z.many_pieces * ROWS_MANY * (c.D + 2)) * 4 + (z.own_items + z.many_items) * 8);
+    z.bytes = (size_t)((z.own_pieces * z.piece_size + z.many_pieces * ROWS_MANY * (c.D + 2)) * 4 + (int64_t)B * c.Hkv * 32 + z.own_items * 8);
     z.fits = z.blocks * 256 <= 0xffffffffLL && (int64_t)B * c.Hkv * ((rows + 3) / 4) <= 0xffffffffLL / 512;
     return z;
 }
@@ -817,8 +801,8 @@ int launch_cache_attn_shared(const CacheView& c, const Rows& q, const Rows& out,
     x.max_own = z.own_pieces;
     a.pieces = (float*)workspace;
     x.pieces = a.pieces + z.own_pieces * z.piece_size;
-    a.split = (int2*)(x.pieces + z.many_pieces * ROWS_MANY * (c.D + 2));
-    x.split = a.split + z.own_items;
+    x.where = (int4*)(x.pieces + z.many_pieces * ROWS_MANY * (c.D + 2));
+    a.split = (int2*)(x.where + 2 * (int64_t)s.B * c.Hkv);
     auto pick = [&](auto D, auto F) { return z.mt == 1 ? launch_shared<D, F != 0, 1>(x, z, stream) : launch_shared<D, F != 0, 2>(x, z, stream); };
     if (c.D == 128) return c.e5m2 ? pick(IC<128>{}, IC<1>{}) : pick(IC<128>{}, IC<0>{});
     return c.e5m2 ? pick(IC<64>{}, IC<1>{}) : pick(IC<64>{}, IC<0>{});
