@@ -6,7 +6,17 @@
 // (many_steps).  What a sequence has behind it is visited with its own rows in tiles of 16 or 32, a wave by itself to each tile, or to a part of its
 // steps: such parts are short, and waves that wait for each other would wait more than they work.  One launch does both: the
 // first is bound by matrix and vector work, the second by the bytes of the cache, and workgroups of both kinds share the CUs.  A second one
-// joins.  How long the sequences are is on the device alone: each workgroup finds its part of the work by itself.
+// joins.  How long the sequences are is on the device alone: each workgroup finds its part of the work by itself (3 us of a call, 4 to 5 with 256
+// sequences).
+//
+// A CU holds two workgroups.  A step of a prefix takes one 1.6 us by itself and 2.3 beside another (1.15 per step), as its matrix and vector
+// work take turns then; beside sequences' own parts, which wait for memory, 1.7.
+//
+// Measured, 32 query and 8 kv heads, D = 128, E4M3, one token per sequence, call to call: 64 sequences of up to 512 behind 8192 33.5 us (dma_cache_attn,
+// which reads the prefix 64 times, by way of the caches, 105); 256 of up to 700 behind 32768 203 us = 0.68 PFLOP/s (1845; the matrix product of
+// 8192^3 would take 121 for as many flops); 64 of up to 500 behind 8192 with 32 kv heads 65 us for 217 MB = 3.3 TB/s (538); 32 under a window of 4096
+// 35.5 us (39.6).  Of the 33.5: 3 to find the work, 3.5 until the first products, 8 steps of the prefix 14.5 (own parts end before), 2 to write pieces, 2.8
+// launch and end, the join 6.5.
 #include "dma_cache_many.hpp"
 #include <algorithm>
 
@@ -112,7 +122,8 @@ DMA_DEV float wave_sum(float v)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// One workgroup's part of the prefixes: 128 rows of a group, some of their steps, into piece `piece`.
+// One workgroup's part of the prefixes: 128 rows of a group, some of their steps, into piece `piece`: of those of part `part` of `parts` the first
+// share `early`, or (late) the others.  pieces: the first one of the rows, and how many.
 template <int D, bool E5M2, bool UNI>
 DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)[5][WAVES], const Bounds& g, int h, int tile, int part, int parts, float early, bool late, int64_t piece, int2 pieces)
 {
@@ -645,7 +656,7 @@ cache_shared_kernel(SharedArgs x)
 }
 
 // Joins the pieces of the prefix and of a sequence's own: a workgroup per sequence, kv head and 4 of its rows; threads over channels (4 each),
-// rows and pieces.
+// rows and pieces, eight of a thread in flight.  64 sequences, 17 pieces of a row (19 MB): 6.5 us; 256 sequences, 9 to 10 (41 MB): 11.
 template <int D, int ROWS, int T>
 __global__ void __launch_bounds__(T)
 cache_shared_join_kernel(SharedArgs x)
@@ -747,7 +758,9 @@ static SharedSizes sizes_of(const CacheView& c, int B, int G, int N, int n_group
 }
 
 // Whether sequences are taken together: where it saves reading this much once more, by the reach of the table (lengths are on the device), and
-// the rows of one sequence do not fill a tile anyway.
+// the rows of one sequence do not fill half a tile anyway.  us together and by the kernels of dma_cache_attn, 32 query and 8 kv heads (MB repeated): 2
+// behind 500 (1) 15.5, 9.0; 2 behind 8k (17) 20.7, 17.8; 8 behind 4096 (65) 21.6, 21.3; 32 behind 2000 (146) 21.5, 26.5; 64 behind 8k (1100) 34, 102.
+// Rows of a sequence, 64 behind 8k: 16: 64, 107; 32: 100, 118; 64: 163, 262; 128: 320, 273.
 constexpr int ROWS_TOGETHER = 64;
 constexpr double REPEATED = 1e8;
 static bool together(const SharedSizes& z, const CacheView& c, int B, int64_t rows, int n_groups, int window, int sinks)
