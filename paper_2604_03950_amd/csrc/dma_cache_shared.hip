@@ -447,12 +447,18 @@ DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& ran
     }
 }
 
-constexpr int MIN_MANY = 2, MIN_OWN = 4;     // steps of a part at least
-// What the sequences' own parts take of a CU's time beside a prefix's part, in steps of that: until a late part begins, and per step.
-constexpr float OWN_FIRST = 6.f, OWN_STEP[2] = {0.6f, 0.9f};      // tiles of 16 and of 32 rows
-// Of the steps that two parts of prefixes do side by side on a CU, those of the one that began later (the SIMDs prefer older waves).
+// Steps of a part at least.  Of a prefix (1, 2, 4, 8 steps), us: 32 sequences behind 4096 23.1, 23.3, 21.0, 26.2; 64 behind 1024 with parts of 2, 3, 4,
+// 6: 22.8, 20.9, 22.2, 24.1.  Of a sequence's own (2, 4, 8), 64 in 16 groups 41.3, 40.3, 43.9; 256 behind 32768 210, 204, 208.
+constexpr int MIN_MANY = 4, MIN_OWN = 4;
+// What the sequences' own parts take of a CU's time beside a prefix's part, in steps of that: until a late part begins, and per step, for tiles of 16 and
+// of 32 rows.  256 behind 32768 with half of them 210 us, with these 204, with twice as much 219.
+constexpr float OWN_FIRST = 6.f, OWN_STEP[2] = {0.6f, 0.9f};
+// Of the steps that two parts of prefixes do side by side on a CU, those of the one that began later (the SIMDs prefer older waves).  128 sequences behind
+// 32768 with 0.375: the early ones end at 92 us, the late ones at 85; 0.42: 90 and 91; 0.5: 74 and 89.
 constexpr float LATE = 0.42f;
-constexpr float MIN_LATE = 3.f;              // steps of a late part at least
+// Steps of a late part at least: without late parts 256 behind 32768 take 239 us (204), 128 of one token behind 32768 116 (98); 64 of up to 512 behind
+// 8192, whose own parts fill that time, 34 either way.  1 or 8 instead of 3: the same within 1 %.
+constexpr float MIN_LATE = 3.f;
 
 // Rows of a sequence: tiles of 16 * MT.
 template <int D, bool E5M2, int MT, bool UNI>
