@@ -307,6 +307,7 @@ int dma_kv_fork(const dma_kv_cache* cache, void* refs_i32, int B, const void* sr
  *   start, n_tokens, N   as for dma_kv_write; positions past max_pages * page_tokens are none.
  *   missing_i32  [B] int32, device, 4-byte aligned, out: entries of the sequence for which no free page was left.  They stay as they were,
  *                and what is written to them would be lost, or be written to a page of others.
+ *   B = 0 or N = 0 is a no-op: missing is not written.
  *   workspace    device, 4-byte aligned, at least dma_kv_reserve_workspace_bytes(...) bytes; as for dma_cache_attn.
  *   B times the pages that N tokens can touch must stay below 2^30 (else DMA_ERR_UNSUPPORTED).
  */

@@ -14,8 +14,9 @@ namespace dma {
 // take over each other's entries in place, and counts there how many rows take over each: what row r named is named (that - 1) times more.
 // One atomic at most per entry that is not taken over exactly once, instead of one for each that goes and one for each that comes.
 //
-// Bound by latency: three trips to memory and LDS one behind the other.  8 rows of 16 entries: 2.7 us; 256 rows of 2048, of which every eighth takes
-// the place of seven: 16 us (2.1 MB of table read and written; with an atomic for each entry that goes or comes, and no LDS, 39 call to call, now 18).
+// 8 rows of 16 entries: 2.7 us, bound by latency (three trips to memory and LDS one behind the other).  256 rows of up to 2048, of which every eighth
+// takes the place of seven: 16 us for 2.1 MB of table; 7 of them are a count read and written for each of 314 000 pages in random places.  (With an
+// atomic for each entry that goes or comes, and no LDS, 39 call to call, now 18; with all loads of a workgroup of 1024 in flight at once 21.)
 __global__ void __launch_bounds__(256)
 kv_fork_kernel(CacheView c, int* table, int* refs, int B, int cols_shift, const int* src, const int* length)
 {
