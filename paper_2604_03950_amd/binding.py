@@ -451,7 +451,7 @@ def dma_kv_reserve(cache: KVCache, refs: torch.Tensor, start: torch.Tensor, N: i
     if not -1 << 31 <= N < 1 << 31:
         raise ValueError("N must be an int of 32 bits")
     if missing is None:
-        missing = torch.zeros(cache._b, dtype=_I32, device=cache.device)
+        missing = (torch.empty if N > 0 else torch.zeros)(cache._b, dtype=_I32, device=cache.device)
     pm = _counts(cache, missing, "missing")
     L = load()
     pw, nw, workspace = _scratch(cache, workspace, 0 if workspace is not None else L.dma_kv_reserve_workspace_bytes(cache._ref, cache.B, N))
@@ -477,7 +477,7 @@ def dma_kv_compact(cache: KVCache, refs: torch.Tensor, *, used: torch.Tensor | N
     pages = cache._c.num_pages
     pr = _ints(cache, refs, pages, "refs")
     if used is None:
-        used = torch.zeros(1, dtype=_I32, device=cache.device)
+        used = torch.empty(1, dtype=_I32, device=cache.device)
     if moved is None:
         moved = torch.empty(pages, dtype=_I32, device=cache.device)
     pu, pm = _ints(cache, used, 1, "used"), _ints(cache, moved, pages, "moved")
