@@ -766,13 +766,15 @@ static SharedSizes sizes_of(const CacheView& c, int B, int G, int N, int n_group
 // Whether sequences are taken together: where it saves reading this much once more, by the reach of the table (lengths are on the device), and
 // the rows of one sequence do not fill half a tile anyway.  us together and by the kernels of dma_cache_attn, 32 query and 8 kv heads (MB repeated): 2
 // behind 500 (1) 15.5, 9.0; 2 behind 8k (17) 20.7, 17.8; 8 behind 4096 (65) 21.6, 21.3; 32 behind 2000 (146) 21.5, 26.5; 64 behind 8k (1100) 34, 102.
-// Rows of a sequence, 64 behind 8k: 16: 64, 107; 32: 100, 118; 64: 163, 262; 128: 320, 273.
-constexpr int ROWS_TOGETHER = 64;
+// Rows of a sequence, 64 behind 8k: 16: 64, 107; 32: 100, 118; 64: 163, 262; 128: 320, 273.  More than 32 rows under a short table, where
+// the other kernels read 128 rows' keys once as well: 170 random calls, geometric mean of the times' ratio: below 600 positions 2.0, to 1200 1.45, to 2500 1.1, to
+// 5000 0.75, behind that 0.95 (up to 32 rows 0.54 to 1.05 everywhere).
+constexpr int ROWS_TOGETHER = 64, ROWS_SHORT = 32, REACH_LONG = 2048;
 constexpr double REPEATED = 1e8;
 static bool together(const SharedSizes& z, const CacheView& c, int B, int64_t rows, int n_groups, int window, int sinks)
 {
     const int64_t capacity = (int64_t)c.max_pages << c.page_shift, reach = window ? std::min(capacity, (int64_t)window + sinks) : capacity;
-    return n_groups > 0 && rows <= ROWS_TOGETHER && (double)(B - n_groups) * reach * 2 * c.Hkv * c.D >= REPEATED && z.fits;
+    return n_groups > 0 && rows <= (reach >= REACH_LONG ? ROWS_TOGETHER : ROWS_SHORT) && (double)(B - n_groups) * reach * 2 * c.Hkv * c.D >= REPEATED && z.fits;
 }
 
 size_t cache_attn_shared_workspace(const CacheView& c, int B, int Hq, int N, int n_groups, int window, int sinks)
