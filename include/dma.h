@@ -259,10 +259,12 @@ int dma_kv_read(const dma_kv_cache* cache, const dma_rows* k_out, const dma_rows
  *   The query at position p sees the keys at positions t <= p and, if window > 0, of these only t > p - window and
  *   t < sink_tokens (the first tokens of the sequence stay visible).  window = 0: no window, sink_tokens has no effect.
  *   A query that sees no key (none of the positions it could see has a page) gives zeros.
- *   Positions that are not seen may hold anything, codes of NaN and infinities among it, and the scale of a page of which no position
- *   is seen may be any byte.  A NaN among the keys that a query sees makes its row NaN, one among the values that channel of it.
- *   An infinity (an E5M2 code that dma_kv_write never leaves) among the values that a query sees makes that channel of its row an
- *   infinity or NaN, which of them unspecified; one among the keys leaves the rows that see it unspecified.
+ *   What a query does not see may hold anything, codes of NaN and infinities among it, and the scale of a page of which it sees no position
+ *   may be any byte, whatever other queries see.  A NaN among the keys that a query sees makes its row NaN, one among the values that channel
+ *   of it; under a scale of 255, the byte of NaN, all elements of the page are NaN.
+ *   An infinity (an E5M2 code that dma_kv_write never leaves, or an element that a scale above those it leaves takes to 2^128) among the
+ *   values that a query sees makes that channel of its row an infinity or NaN, which of them unspecified; one among the keys leaves the
+ *   rows that see it unspecified.
  * Scores, softmax statistics and sums are binary32; probabilities are rounded to bf16 for the second product, as in dma_attn_fwd,
  * and the sum that divides them adds the rounded ones.  The sums are divided at the end: they hold n keys' values of up to
  * 2^121 / (n + 64) in magnitude; larger ones, which the cache can hold, may give infinities or NaN though their mean is finite.  The

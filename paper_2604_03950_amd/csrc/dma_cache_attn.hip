@@ -361,6 +361,8 @@ cache_attn_kernel(CacheAttnArgs a)
                 // through a probability of zero: zeros instead, and NaN in the sums of those who see it.  Nor may the scale of a page of which
                 // no row sees anything, or of page 0 in the place of none: with 255 a zero is decoded to NaN
                 if (!any) v_scale = 127;
+                const unsigned limit = no_number_limit<E5M2>(v_scale);
+                if (v_scale == 255) v_scale = 127;                // (no code stays)
                 bool bad = false;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -368,7 +370,7 @@ cache_attn_kernel(CacheAttnArgs a)
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
                         vr[dt][w] &= keep;
-                        const unsigned f = no_number<E5M2>((unsigned)vr[dt][w]);
+                        const unsigned f = no_number((unsigned)vr[dt][w], limit);
                         if (f) bad = true;
                         vr[dt][w] &= (int)~((f >> 7) * 0xffu);
                     }

@@ -100,10 +100,17 @@ DMA_DEV int pack_bf16(float a, float b)
     return __builtin_bit_cast(int, r);
 }
 
-// Bytes that are no number (NaN, infinity): bit 7 of each.  Both are put into the sums as NaN where a step is masked; in the others an
-// infinity goes through the products as one.
+// Codes that are no number under their page's scale: bit 7 of each byte.  NaN and infinity in the format, from its code `least` on; under a scale above
+// those that a write leaves, also what reaches 2^128, which bf16 does not hold: an exponent field of 128 + bias - (scale - 127); with 255, the
+// byte of NaN, every code.  All are put into the sums as NaN where a step is masked; in the others an infinity goes through the products as one.
+// limit: what brings the codes from there on to bit 7 when it is added to each.
 template <bool E5M2>
-DMA_DEV unsigned no_number(unsigned w) { return ((w & 0x7f7f7f7fu) + (E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u; }
+DMA_DEV unsigned no_number_limit(int scale)
+{
+    constexpr int least = E5M2 ? 0x7c : 0x7f, bias = E5M2 ? 15 : 7, mantissa = E5M2 ? 2 : 3;
+    return (unsigned)(128 - (scale == 255 ? 0 : min(least, (255 + bias - scale) << mantissa))) * 0x01010101u;
+}
+DMA_DEV unsigned no_number(unsigned w, unsigned limit) { return ((w & 0x7f7f7f7fu) + limit) & 0x80808080u; }
 
 // Bits 0 to 3 -> the four bytes of a dword.
 DMA_DEV int bytes_of(unsigned bits) { return (int)((((bits & 15u) * 0x00204081u) & 0x01010101u) * 0xffu); }
@@ -122,12 +129,14 @@ DMA_DEV unsigned long long nan_channels(const CacheAttnArgs& a, int b, int h, in
         if ((unsigned)page >= a.c.page_limit) continue;
         auto below = [&](int at) { return (1u << min(max(at - p, 0), 16)) - 1u; };
         const unsigned seen = below(vis_hi + 1) & (~below(vis_lo) | below(a.sinks));
-        const uint8_t* base = a.c.v_codes + (((((int64_t)page * a.c.Hkv + h) * D) << a.c.page_shift) + (p & ((1 << a.c.page_shift) - 1)));
+        const int64_t slab = (int64_t)page * a.c.Hkv + h;
+        const uint8_t* base = a.c.v_codes + (((slab * D) << a.c.page_shift) + (p & ((1 << a.c.page_shift) - 1)));
+        const unsigned limit = no_number_limit<E5M2>(a.c.v_scales[slab]);
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
             const v4i w = *(const v4i*)(base + (channel(i) << a.c.page_shift));
             unsigned bad = 0;
-            for (int k = 0; k < 4; ++k) bad |= no_number<E5M2>((unsigned)w[k]) & (unsigned)bytes_of(seen >> (4 * k));
+            for (int k = 0; k < 4; ++k) bad |= no_number((unsigned)w[k], limit) & (unsigned)bytes_of(seen >> (4 * k));
             if (bad) hit |= 1ull << i;
         }
     }

@@ -128,7 +128,7 @@ DMA_DEV void many_steps(const CacheAttnArgs& a, const ManyLds<D>& lds, int b, in
 #pragma unroll
         for (int u = 0; u < VCH; ++u) {
             const int ch = threadIdx.x + u * T, d = channel_of(ch);
-            float sc = __int_as_float(cd.vsc[UNI ? 0 : u] << 23);
+            int scale = cd.vsc[UNI ? 0 : u];
             const bool there = cd.there[UNI ? 0 : u];
             if (!there) odd |= 1 << (ch & 3);
             if (!open || !there) {
@@ -140,15 +140,18 @@ DMA_DEV void many_steps(const CacheAttnArgs& a, const ManyLds<D>& lds, int b, in
                     for (int w = 0; w < NW; ++w) some |= lds.some[(j & 3) * NW + w];
                     if (a.window && !((some >> (ch & 3)) & 1)) seen = 0;
                 }
-                if (!seen) sc = 1.f;
+                if (!seen) scale = 127;
+                const unsigned limit = no_number_limit<E5M2>(scale);
+                if (scale == 255) scale = 127;                     // (no code stays)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     cd.v[u][w] &= bytes_of(seen >> (4 * w));
-                    const unsigned bad = no_number<E5M2>((unsigned)cd.v[u][w]);
+                    const unsigned bad = no_number((unsigned)cd.v[u][w], limit);
                     if (bad) odd |= 16;
                     cd.v[u][w] &= (int)~((bad >> 7) * 0xffu);
                 }
             }
+            const float sc = __int_as_float(scale << 23);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
                 *(v8bf*)(lds.v[buf] + d * VROW + ((2 * (ch & 3) + e) ^ shift_of(d, VROW)) * 16) = decode8<E5M2>(cd.v[u][2 * e], cd.v[u][2 * e + 1], sc);

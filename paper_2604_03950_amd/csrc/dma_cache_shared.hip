@@ -365,6 +365,8 @@ DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& ran
             // values that no row sees may be anything, the scale of their page too, and a NaN among the others must not reach the rows that do
             // not see it through a probability of zero: zeros instead, and NaN in the sums of those who see it
             if (!any) v_scale = 127;
+            const unsigned limit = no_number_limit<E5M2>(v_scale);
+            if (v_scale == 255) v_scale = 127;                    // (no code stays)
             bool bad = false;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -372,7 +374,7 @@ DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& ran
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
                     vr[dt][w] &= keep;
-                    const unsigned f = no_number<E5M2>((unsigned)vr[dt][w]);
+                    const unsigned f = no_number((unsigned)vr[dt][w], limit);
                     if (f) bad = true;
                     vr[dt][w] &= (int)~((f >> 7) * 0xffu);
                 }
