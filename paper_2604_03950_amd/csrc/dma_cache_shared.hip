@@ -587,14 +587,17 @@ cache_shared_kernel(SharedArgs x)
         const int own_blocks = min((all_units + WAVES - 1) / WAVES, max(2 * x.cus - 8 * per, x.cus));
         p -= 8 * per;
         if (p < own_blocks) {
+            // A wave's units only grow: each is looked for from the batch of sequences on that holds the one before it.  (From the first on, 16384
+            // sequences of one token behind 512 took 9600 us.)
+            int base = 0, before = 0;                             // the batch in the registers, and the units before it
+            if (a.s.B > 256) {
+                load4(base, false);
+                count4(base);
+            }
             for (int unit = p * WAVES + wave; unit < all_units; unit += own_blocks * WAVES) {
-                int left = unit, b = -1, per_head = 1;
+                int left = unit - before, b = -1, per_head = 1;
                 OwnSeq sq = {0, 0, 0};
-                for (int base = 0; base < a.s.B && b < 0; base += 256) {
-                    if (a.s.B > 256) {
-                        load4(base, false);
-                        count4(base);
-                    }
+                for (;;) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         if (base + 64 * k >= a.s.B || b >= 0) continue;
@@ -611,6 +614,11 @@ cache_shared_kernel(SharedArgs x)
                         per_head = __builtin_amdgcn_readlane(units[k], who);
                         left -= (__builtin_amdgcn_readlane(upto[k], who) - per_head) * a.c.Hkv;
                     }
+                    if (b >= 0 || base + 256 >= a.s.B) break;
+                    before = unit - left;
+                    base += 256;
+                    load4(base, false);
+                    count4(base);
                 }
                 if (b < 0) break;
                 const int h = left / per_head;

@@ -138,3 +138,18 @@ def test_large_batches_of_several_tokens(fmt, D, P, G, N, B):
     f, lens = family_of_many(rng, sizes + [B - sum(sizes) - 4], 2, 1, P, D, fmt, N, [200, 400])
     n = np.where(rng.random(B) < 0.2, 0, rng.integers(1, N + 1, B))
     check(f, bf16(rng, B, G, N, D), lens - N, n)
+
+
+@pytest.mark.parametrize("fmt,D,P,Hkv,G,N", [("e4m3", 64, 64, 8, 2, 1), ("e5m2", 128, 32, 4, 4, 5)])
+@pytest.mark.parametrize("B", [700, 1537])
+def test_several_parts_of_large_batches_for_a_wave(fmt, D, P, Hkv, G, N, B):
+    """More parts of sequences' own than there are waves, in batches of 256 sequences that a wave goes on through; sequences without tokens, among
+    them whole batches at the front, in the middle and at the end."""
+    rng = np.random.default_rng(B + N)
+    sizes = [300, 1, 0, 90]
+    f, lens = family_of_many(rng, sizes + [B - sum(sizes) - 6], 3, Hkv, P, D, fmt, N, [64, 130])
+    for gone in ([], [(256, 600)], [(0, 300), (B - 260, B)]):
+        n = np.where(rng.random(B) < 0.1, 0, rng.integers(1, N + 1, B))
+        for lo, hi in gone:
+            n[lo:hi] = 0
+        check(f, bf16(rng, B, Hkv * G, N, D), lens - N, n)
