@@ -781,10 +781,19 @@ static SharedSizes sizes_of(const CacheView& c, int B, int G, int N, int n_group
 // 5000 0.75, behind that 0.95 (up to 32 rows 0.54 to 1.05 everywhere).
 constexpr int ROWS_TOGETHER = 64, ROWS_SHORT = 32, REACH_LONG = 2048;
 constexpr double REPEATED = 1e8;
+// Every workgroup goes through the batch and the groups to find its part: 5 ns of a call's time per workgroup and 256 sequences or 26 groups, but for the
+// first 2500 of them, which run side by side.  The other kernels take 8 ns more per sequence and kv head.  Both as bytes that those would read
+// again meanwhile, from the caches mostly (13 TB/s).  us together and by the other kernels, D = 128, one token: 4096 sequences behind 512 in one group, 8 kv
+// heads of 4 query heads, 515, 980; in 1024 groups 5902, 1007; 16384 in one group, 1 kv head of 8, behind 4300 1611, 1654, behind 1000 1391, 639.  Of 612 calls
+// of 200 to 16384 sequences in 1 to 2048 groups, 542 repeat 100 MB: 1.08 of the other kernels' time (geometric mean, 0.17 to 15.9); 139 of these are not taken
+// together for this (2.5, 0.90 to 15.9), which leaves 0.81 (0.17 to 2.5; above 1.3 with few bytes of a sequence per kv head or 16 and 32 rows).
+constexpr double FINDING = 8e4, FINDING_FREE = 2500, ITEM = 1e5, GROUP = 10;
 static bool together(const SharedSizes& z, const CacheView& c, int B, int64_t rows, int n_groups, int window, int sinks)
 {
     const int64_t capacity = (int64_t)c.max_pages << c.page_shift, reach = window ? std::min(capacity, (int64_t)window + sinks) : capacity;
-    return n_groups > 0 && rows <= (reach >= REACH_LONG ? ROWS_TOGETHER : ROWS_SHORT) && (double)(B - n_groups) * reach * 2 * c.Hkv * c.D >= REPEATED && z.fits;
+    const double finding = FINDING * (z.blocks * (B + GROUP * n_groups) / 256 - FINDING_FREE) - ITEM * z.own_items;
+    return n_groups > 0 && rows <= (reach >= REACH_LONG ? ROWS_TOGETHER : ROWS_SHORT) &&
+           (double)(B - n_groups) * reach * 2 * c.Hkv * c.D >= REPEATED + std::max(finding, 0.0) && z.fits;
 }
 
 size_t cache_attn_shared_workspace(const CacheView& c, int B, int Hq, int N, int n_groups, int window, int sinks)

@@ -9,7 +9,7 @@ import kv_counts
 import kv_rows
 from paper_2604_03950_amd import binding as dma
 from test_gpu_cache_attn_shared import Family
-from test_gpu_kv_cache import bf16, i32
+from test_gpu_kv_cache import FMT, bf16, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -104,7 +104,11 @@ def family_of_many(rng, sizes, alone, Hkv, P, D, fmt, N, prefixes):
     groups = [(alone, -1)] + [(s, int(rng.choice(prefixes))) for s in sizes] + [(alone, -1)]
     lens = np.concatenate([np.full(s, max(c, 0)) for s, c in groups]).astype(int)
     lens += rng.integers(N, 90, len(lens))
-    return Family(rng, groups, [int(x) for x in lens], Hkv, P, D, fmt), lens
+    f = Family(rng, groups, [int(x) for x in lens], Hkv, P, D, fmt)
+    # a table so wide that so many sequences and groups come to the kernel
+    columns, g = int(2e10 / ((len(lens) - len(f.shared)) * P * 2 * Hkv * D)) + 1, f.gpu
+    f.gpu = dma.KVCache(g.k_codes, g.v_codes, g.k_scales, g.v_scales, torch.nn.functional.pad(g.page_table, (0, columns), value=-1), FMT[fmt])
+    return f, lens
 
 
 @pytest.mark.parametrize("fmt,D,P,Hkv,G,N", [("e4m3", 128, 64, 1, 4, 1), ("e5m2", 64, 32, 2, 5, 5), ("e4m3", 128, 16, 1, 1, 20)])
