@@ -271,7 +271,9 @@ int dma_kv_read(const dma_kv_cache* cache, const dma_rows* k_out, const dma_rows
  * sums q k^T have to stay below 2^127.
  * Equal calls give equal bits; the order of the sums over the keys follows from the sizes and the values of start and n_tokens.
  *   workspace  device, 16-byte aligned, at least dma_cache_attn_workspace_bytes(...) bytes (NULL if that is 0); not
- *              initialised by the caller, without meaning after the call.  Calls that may run at the same time need one each.
+ *              initialised by the caller, without meaning after the call.  Calls that may run at the same time need one each.  The bytes are
+ *              those of a call with just these arguments: the kernels change with the sizes, and fewer sequences, tokens or positions, or
+ *              another window, may need more.  A caller who keeps one workspace takes the largest over the calls it will make.
  */
 int dma_cache_attn(const dma_kv_cache* cache, const dma_rows* q, const dma_rows* out, int B, int Hq, int N, const void* start_i32,
                    const void* n_tokens_i32, int window, int sink_tokens, void* workspace, size_t workspace_bytes, void* stream);
@@ -282,6 +284,8 @@ size_t dma_cache_attn_workspace_bytes(const dma_kv_cache* cache, int B, int Hq, 
 
 /*
  * Pages that several sequences hold, and who holds what.
+ *
+ * (A call's outputs and its workspace lie apart from each other and from all that it reads.)
  *
  * Rows of the page table may name the same page.  refs [num_pages] int32 (device, 4-byte aligned) says of every page how many entries of
  * the table name it; a page of which it says 0 is free.  A caller that begins with a table of -1 and refs of 0 and changes both only by the
@@ -305,7 +309,8 @@ int dma_kv_fork(const dma_kv_cache* cache, void* refs_i32, int B, const void* sr
  * page, or a page with refs > 1, becomes a free page; the r-th of these entries, sequence by sequence and in order of position, the r-th
  * free page in ascending order (refs as they were before the call say what is shared and what is free).  Where the sequence has earlier
  * tokens in a shared page (its first one, start not a multiple of page_tokens), the codes and scales of the whole page are copied; any other
- * page that is handed out holds nothing (scales of 255).  Every sequence that shares a page it asks for leaves it; none keeps it.
+ * page that is handed out holds nothing (scales of 255).  Every sequence that shares a page it asks for leaves it; none keeps it: n samples of
+ * one prompt that part in one call need n free pages, and the page they leave, named by nobody else, is free for the next call.
  *   start, n_tokens, N   as for dma_kv_write; positions past max_pages * page_tokens are none.
  *   missing_i32  [B] int32, device, 4-byte aligned, out: entries of the sequence for which no free page was left.  They stay as they were,
  *                and what is written to them would be lost, or be written to a page of others.
@@ -336,7 +341,11 @@ size_t dma_kv_compact_workspace_bytes(const dma_kv_cache* cache);
  *   group_start[g + 1] (not included), of the B.  A sequence may be in no group.
  *   shared [n_groups] int32, device, 4-byte aligned: the positions [0, shared[g]) of all sequences of group g that have tokens are the same: their rows
  *   of the table name the same pages there (or pages that hold the same).  Below 1: none.
- *   Everything else is as for dma_cache_attn, and so is what the call computes; the order of its sums differs, and so may the last bits.
+ *   Everything else is as for dma_cache_attn, and so is what the call computes; the order of its sums differs, and so may the last bits.  The
+ *   workspace too: more groups may need less.
+ *   Lengths are on the device: whether the prefix is read once or the kernels of dma_cache_attn serve the call follows from the sizes (sequences, groups, kv
+ *   heads, positions of the table or of the window), as if all of the table were full.  Under a table much wider than the sequences the call
+ *   may take longer than dma_cache_attn.
  * A group_start that decreases gives unspecified results, never a fault.  With n_groups = 0 the two arrays are not looked at (may be NULL).
  * n_groups > 2^24: DMA_ERR_UNSUPPORTED.
  */

@@ -403,7 +403,8 @@ def dma_cache_attn(q: torch.Tensor, cache: KVCache, start: torch.Tensor, n_token
 
 
 def dma_cache_attn_workspace_bytes(cache: KVCache, Hq: int, N: int, window: int = 0, sink_tokens: int = 0) -> int:
-    """Bytes of workspace of a dma_cache_attn call with q [B, Hq, N, D] on the current device."""
+    """Bytes of workspace of a dma_cache_attn call with q [B, Hq, N, D] on the current device; of just this call: fewer tokens, or another
+    window, may need more."""
     return int(load().dma_cache_attn_workspace_bytes(cache._ref, cache.B, Hq, N, window, sink_tokens))
 
 
@@ -528,7 +529,8 @@ def dma_cache_attn_shared(q: torch.Tensor, cache: KVCache, start: torch.Tensor, 
 
 
 def dma_cache_attn_shared_workspace_bytes(cache: KVCache, Hq: int, N: int, n_groups: int, window: int = 0, sink_tokens: int = 0) -> int:
-    """Bytes of workspace of a dma_cache_attn_shared call with q [B, Hq, N, D] and n_groups groups on the current device."""
+    """Bytes of workspace of a dma_cache_attn_shared call with q [B, Hq, N, D] and n_groups groups on the current device; of
+    just this call: fewer tokens or groups, or another window, may need more."""
     return int(load().dma_cache_attn_shared_workspace_bytes(cache._ref, cache.B, Hq, N, n_groups, window, sink_tokens))
 
 

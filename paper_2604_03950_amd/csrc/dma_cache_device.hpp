@@ -26,7 +26,7 @@ struct CacheAttnArgs {
     int parts;               // many rows: pieces of an item at most, side by side
 };
 
-// A word of a table that no kernel writes, at an index that is the same for all lanes: by way of the scalar cache, whose loads are counted
+// A word of a table that no kernel running at the same time writes, at an index that is the same for all lanes: by way of the scalar cache, whose loads are counted
 // apart from those of the codes.
 DMA_DEV int scalar_at(const int* table, int index)
 {

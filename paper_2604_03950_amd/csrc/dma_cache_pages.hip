@@ -15,7 +15,8 @@ namespace dma {
 // One atomic at most per entry that is not taken over exactly once, instead of one for each that goes and one for each that comes.
 //
 // 8 rows of 16 entries: 2.7 us, bound by latency (three trips to memory and LDS one behind the other).  256 rows of up to 2048, of which every eighth
-// takes the place of seven: 16 us for 2.1 MB of table; 7 of them are a count read and written for each of 314 000 pages in random places.  (With an
+// takes the place of seven: 16 us for 2.1 MB of table; 7 of them are a count read and written for each of 314 000 pages in random places, 9 the table, of
+// whose lines of 128 bytes a workgroup has 16: 29 MB are read for 4.2.  (With an
 // atomic for each entry that goes or comes, and no LDS, 39 call to call, now 18; with all loads of a workgroup of 1024 in flight at once 21.)
 __global__ void __launch_bounds__(256)
 kv_fork_kernel(CacheView c, int* table, int* refs, int B, int cols_shift, const int* src, const int* length)
@@ -125,7 +126,8 @@ constexpr int NOT_GIVEN = -1, GIVEN_NEW = -2;      // in the workspace, per entr
 // follows from the entries before it alone, so that equal calls give equal tables: sums over the workgroup instead of atomics.
 //
 // Bound by latency: start, entry, refs of the page, sums, refs of the free pages, one behind the other.  64 sequences with a token each: 3.6 us;
-// 13 with up to 4100 tokens in pages of 32: 6.5; 256 with one each: 4.3.
+// 13 with up to 4100 tokens in pages of 32: 6.5; 256 with one each: 4.3.  Pages are looked at from the first on, 4096 per turn of 1.2 us: where the first 130 000 of
+// 131 072 are used, both kernels take 48 us call to call, 8.5 where the first 8000 hold a free one.
 __global__ void __launch_bounds__(1024)
 kv_reserve_kernel(CacheView c, int* table, int* refs, Spans s, int pages_per_seq, int* missing, int* left)
 {
@@ -248,7 +250,7 @@ struct Moves {
 size_t compact_workspace(const CacheView& c) { return 8 + 8 * (size_t)(c.num_pages / 2); }
 
 // One workgroup: counts, then lists free pages below the count and used ones from there on.  In order, so that equal calls give equal tables.
-// Bound by latency: 300 pages 3.6 us, 4096 pages 6.1.
+// Bound by latency: 300 pages 3.6 us, 4096 pages 6.1, 131 072 (call to call, nothing to move) 107.
 __global__ void __launch_bounds__(1024)
 kv_compact_plan_kernel(CacheView c, const int* refs, int* used_out, int* moved, Moves* moves)
 {

@@ -7,7 +7,7 @@
 // steps: such parts are short, and waves that wait for each other would wait more than they work.  One launch does both: the
 // first is bound by matrix and vector work, the second by the bytes of the cache, and workgroups of both kinds share the CUs.  A second one
 // joins.  How long the sequences are is on the device alone: each workgroup finds its part of the work by itself (3 us of a call, 4 to 5 with 256
-// sequences).
+// sequences, and from there on by the number of workgroups times that of sequences and groups: some 250 of 515 us with 4096 sequences of one group).
 //
 // A CU holds two workgroups.  A step of a prefix takes one 1.6 us by itself and 2.3 beside another (1.15 per step), as its matrix and vector
 // work take turns then; beside sequences' own parts, which wait for memory, 1.7.
@@ -207,7 +207,8 @@ DMA_DEV void prefix_part(const SharedArgs& x, const ManyLds<D>& lds, int (&ends)
 
 // One wave's part of what a sequence has to itself: steps [begin, end) for a tile of 16 * MT of its rows, into a piece.  S^T = K Q^T with the keys in
 // an order that leaves every probability in the lane that needs it for O^T = V^T P^T, one maximum per row that is raised only where it was far too
-// low, codes of the next step on their way while one is worked on: as in the kernel for few rows (dma_cache_attn.hip), whose comments say why.
+// low, codes of the next step on their way while one is worked on: as in the kernel for few rows (dma_cache_attn.hip), whose comments say why.  (Its loop
+// written once more: as one function for both, that kernel's instructions changed.  What is mended in one is mended in the other.)
 // qs: with 32 rows, room for the queries' operands in LDS.
 template <int D, bool E5M2, int MT, bool UNI>
 DMA_DEV void own_part(const SharedArgs& x, const OwnSeq& sq, const OwnRange& range, int b, int h, int tile, int begin, int end, int64_t piece, v8bf* qs)
@@ -458,8 +459,10 @@ constexpr float OWN_FIRST = 6.f, OWN_STEP[2] = {0.6f, 0.9f};
 // Of the steps that two parts of prefixes do side by side on a CU, those of the one that began later (the SIMDs prefer older waves).  128 sequences behind
 // 32768 with 0.375: the early ones end at 92 us, the late ones at 85; 0.42: 90 and 91; 0.5: 74 and 89.
 constexpr float LATE = 0.42f;
-// Steps of a late part at least: without late parts 256 behind 32768 take 239 us (204), 128 of one token behind 32768 116 (98); 64 of up to 512 behind
-// 8192, whose own parts fill that time, 34 either way.  1 or 8 instead of 3: the same within 1 %.
+// Steps of a late part at least: without late parts 256 behind 32768 take 239 us (204), 128 of one token behind 32768 116 (98); 1 or 8 instead of 3: the
+// same within 1 % there.  64 of up to 512 behind 8192 have none by any of these, their own parts being counted as 11.9 steps beside 8 of the prefix: with a
+// tenth to four tenths of the steps made late against that, 40 to 41 us instead of 33, and 32 under a window of 4096 37 to 38 instead of 35; each row then
+// has twice the pieces to write and to join.
 constexpr float MIN_LATE = 3.f;
 
 // Rows of a sequence: tiles of 16 * MT.
@@ -776,6 +779,8 @@ static SharedSizes sizes_of(const CacheView& c, int B, int G, int N, int n_group
 // Whether sequences are taken together: where it saves reading this much once more, by the reach of the table (lengths are on the device), and
 // the rows of one sequence do not fill half a tile anyway.  us together and by the kernels of dma_cache_attn, 32 query and 8 kv heads (MB repeated): 2
 // behind 500 (1) 15.5, 9.0; 2 behind 8k (17) 20.7, 17.8; 8 behind 4096 (65) 21.6, 21.3; 32 behind 2000 (146) 21.5, 26.5; 64 behind 8k (1100) 34, 102.
+// Under a table far wider than the sequences it chooses wrongly: 4 behind 1000 under one for 32768 16.6, 14.5 (by a table of their own width 10.7), 32 behind
+// 300 18.9, 16.9.
 // Rows of a sequence, 64 behind 8k: 16: 64, 107; 32: 100, 118; 64: 163, 262; 128: 320, 273.  More than 32 rows under a short table, where
 // the other kernels read 128 rows' keys once as well: 170 random calls, geometric mean of the times' ratio: below 600 positions 2.0, to 1200 1.45, to 2500 1.1, to
 // 5000 0.75, behind that 0.95 (up to 32 rows 0.54 to 1.05 everywhere).
